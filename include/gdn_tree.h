@@ -75,7 +75,8 @@ enum gdn_status {
     GDN_ERR_DEPTH = -8,       /* a root path has more than max_depth nodes                    */
     GDN_ERR_PATH = -9,        /* accepted path is not a root chain of its tree, or too long   */
     GDN_ERR_WORKSPACE = -10,  /* workspace pointer missing or smaller than required           */
-    GDN_ERR_TIMEOUT = -11     /* a bounded device-side wait expired                           */
+    GDN_ERR_TIMEOUT = -11,    /* a bounded device-side wait expired                           */
+    GDN_ERR_PAGE = -12        /* a page id or a length lies outside the cache                 */
 };
 
 #define GDN_MAX_HEAD_DIM 128   /* d_k, d_v <= 128                     */
@@ -353,6 +354,124 @@ int gdn_tree_verify_static(const gdn_shape_t *shape, const float *S0, const void
                            const void *v, const void *g, const void *beta, const int32_t *parent,
                            const int32_t *node_offsets, void *o, int32_t *status_dev,
                            void *cuda_stream);
+
+/*
+ * Full-attention layers and the output layer of a decode step.  A model that has GDN layers has layers of softmax
+ * attention between them and samples tokens behind them; the draft tree that gdn_tree_verify evaluates at the GDN
+ * layers is evaluated there by gdn_attn_tree_verify, and the accepted path that gdn_tree_commit replays is written by
+ * gdn_kv_commit.  Keys and values live in a paged cache that the caller owns:
+ *   token t of sequence b is in page page_table[b][t / page_size] at place t % page_size; its element e of head h is
+ *   k_cache[page * page_stride + place * token_stride + h * head_stride + e], and v_cache alike (strides in elements, multiples of 16 bytes,
+ *   so that [page][token][head][d], [page][head][token][d] and caches of several layers in one allocation all fit).
+ *   page_table   [device] int32 [n_seq][max_pages]; entries behind a sequence's last token are not read
+ *   seq_lens     [device] int32 [n_seq]: tokens of sequence b that are in the cache (committed, for the calls with rows)
+ *   row_offsets  [device] int32 [n_seq + 1], row_offsets[0] = 0: rows of the call, packed as node_offsets packs nodes;
+ *                sequences without rows are fine
+ *   parent       [device] int32 [total_rows], as for gdn_tree_verify, or NULL: the rows of a sequence follow one another
+ *                (a linear draft, or a chunk of a prompt); max_rows <= GDN_MAX_TREE_NODES with parents
+ *   rows of q, k, v lie q_stride, k_stride, v_stride elements apart (a fused projection can be passed as it is);
+ *                o and q_out are packed [total_rows][h_q][d]
+ * Query head h uses key/value head h / (h_q / h_kv).  All offsets into the cache are formed in 64 bits.  Everything
+ * data-dependent (lengths, pages, trees) lives in device arrays: a captured call can be replayed after they have changed
+ * within max_rows, max_len and total_rows.  Nothing behind row_offsets[n_seq] is written.
+ * Device-side faults: GDN_ERR_TREE (bad row_offsets or parent[]) and GDN_ERR_PAGE for a length that is negative or, with
+ * the call's rows, above max_len: nothing of that sequence is written (by gdn_kv_append: none of its rows on a broken root path);
+ * GDN_ERR_PAGE for a page id outside 0 .. n_pages - 1: the rows that
+ * should go there are not written, tokens that should be read there count as zero vectors (the outputs of that sequence are
+ * then not to be used); GDN_ERR_PATH: no row of that sequence is written.
+ */
+typedef struct gdn_attn_shape {
+    int32_t n_seq;        /* B: sequences                                                          */
+    int32_t h_q;          /* query heads, a multiple of h_kv                                       */
+    int32_t h_kv;         /* key/value heads                                                       */
+    int32_t d;            /* components of a head, a multiple of 8, <= GDN_MAX_HEAD_DIM            */
+    int32_t dtype;        /* gdn_dtype of q, k, v, o and of the cache                              */
+    int32_t total_rows;   /* rows of the call, at least row_offsets[n_seq]; decode: n_seq          */
+    int32_t max_rows;     /* upper bound on the rows of any one sequence; decode: 1                */
+    int32_t n_pages;      /* pages of the cache                                                    */
+    int32_t page_size;    /* tokens of a page, any number                                          */
+    int32_t max_pages;    /* entries of a row of page_table                                        */
+    int32_t max_len;      /* upper bound on the tokens of any one sequence, rows of the call included, <= max_pages * page_size */
+    float scale;          /* multiplies q.k, usually 1/sqrt(d)                                     */
+    int64_t page_stride, token_stride, head_stride;   /* of both caches                            */
+    int64_t q_stride, k_stride, v_stride;             /* >= h_q * d, h_kv * d, h_kv * d            */
+} gdn_attn_shape_t;
+
+/* Bytes of device scratch of gdn_attn_decode and gdn_attn_tree_verify for this shape; 0 if it is invalid.  Contents before and
+ * after a call do not matter; calls that may run at the same time need a workspace each. */
+size_t gdn_attn_workspace_bytes(const gdn_attn_shape_t *shape);
+
+/*
+ * Row i of sequence b goes to token seq_lens[b] + i of the cache: its key rotated by its position, its value as it is.
+ * The position is seq_lens[b] plus the number of the row's proper ancestors (parent NULL: plus i), so that the nodes of
+ * a draft tree stand where they would if they were accepted.  q, rotated alike, goes to q_out; both NULL: keys and values alone.
+ * q_out = q is fine where q is packed.  seq_lens is not changed.
+ *   rope         [device] fp32 [rope_len][rope_dim]: row t holds the cosines of the rope_dim / 2 angles of position t, then
+ *                their sines; rope_len >= max_len; rope_dim even, <= d; components behind it are copied; rope_dim = 0:
+ *                nothing is rotated (rope may be NULL)
+ *   interleaved  0: component i pairs with i + rope_dim / 2; otherwise 2i with 2i + 1
+ */
+int gdn_kv_append(const gdn_attn_shape_t *shape, const void *q, const void *k, const void *v, const float *rope,
+                  int32_t rope_len, int32_t rope_dim, int32_t interleaved, const int32_t *parent,
+                  const int32_t *row_offsets, const int32_t *seq_lens, const int32_t *page_table, void *q_out,
+                  void *k_cache, void *v_cache, int32_t *status_dev, void *cuda_stream);
+
+/*
+ * The counterpart of gdn_tree_commit: the rows of the accepted path path[path_offsets[b] .. path_offsets[b+1]) of each
+ * sequence's tree go to tokens seq_lens[b], seq_lens[b] + 1, ... of the cache, rotated by those positions.  k and v are
+ * the rows as gdn_kv_append was given them (not rotated); what it had written for rejected nodes is overwritten or lies behind the new
+ * length.  The caller adds the paths' lengths to seq_lens afterwards.  parent may be NULL: then only the order of a path is checked.
+ */
+int gdn_kv_commit(const gdn_attn_shape_t *shape, const void *k, const void *v, const float *rope, int32_t rope_len,
+                  int32_t rope_dim, int32_t interleaved, const int32_t *parent, const int32_t *row_offsets,
+                  const int32_t *path, const int32_t *path_offsets, const int32_t *seq_lens,
+                  const int32_t *page_table, void *k_cache, void *v_cache, int32_t *status_dev, void *cuda_stream);
+
+/*
+ * Attention of one new token per sequence: o[b] = softmax(scale q[b] K^T) V over the seq_lens[b] tokens of sequence b, which
+ * the new one is among once gdn_kv_append has written it.  q, o: [n_seq][h_q][d].  A sequence of length 0 gets zeros.
+ *   workspace    : [device], >= gdn_attn_workspace_bytes(shape) bytes, 256-byte aligned
+ */
+int gdn_attn_decode(const gdn_attn_shape_t *shape, const void *q, const void *k_cache, const void *v_cache,
+                    const int32_t *page_table, const int32_t *seq_lens, void *o, void *workspace,
+                    size_t workspace_bytes, int32_t *status_dev, void *cuda_stream);
+
+/*
+ * Attention of the nodes of a draft tree (or of a chunk of a prompt, parent NULL): row i of sequence b sees its seq_lens[b]
+ * committed tokens, its ancestors and itself, row j being token seq_lens[b] + j of the cache, where gdn_kv_append put it.
+ * Nodes that a row does not see have no influence on it, whatever their values.
+ */
+int gdn_attn_tree_verify(const gdn_attn_shape_t *shape, const void *q, const void *k_cache, const void *v_cache,
+                         const int32_t *page_table, const int32_t *seq_lens, const int32_t *parent,
+                         const int32_t *row_offsets, void *o, void *workspace, size_t workspace_bytes,
+                         int32_t *status_dev, void *cuda_stream);
+
+#define GDN_SAMPLE_MAX_VOCAB (1 << 18)
+
+typedef struct gdn_sample_shape {
+    int32_t n_rows;       /* rows of logits                                    */
+    int32_t vocab;        /* logits of a row, <= GDN_SAMPLE_MAX_VOCAB          */
+    int32_t dtype;        /* gdn_dtype of the logits                           */
+    int32_t reserved;     /* 0                                                 */
+    int64_t row_stride;   /* elements between rows, >= vocab; rows need no alignment beyond their type's */
+} gdn_sample_shape_t;
+
+/*
+ * One token per row of logits, from a given random number: the target's tokens at the nodes of a tree, or the next token of each
+ * sequence.  Per row: logits / temperature; of the tokens in descending order (equal logits: the lowest index first) the first top_k;
+ * of those the ones in front of which less than top_p of their probability has gathered (one at least); of those the ones with at
+ * least min_p times the probability of the likeliest.  token is the first kept one, by index, at which the kept tokens'
+ * probability, summed by index and normalised, exceeds uniform; prob (may be NULL) is that token's probability among the kept ones.
+ *   temperature, top_p, min_p : [device] fp32 [n_rows] or NULL (1, off, off); top_k : [device] int32 [n_rows] or NULL (off)
+ *   uniform      [device] fp32 [n_rows] in [0, 1) (clamped to it; NaN: 0)
+ *   temperature <= 0 or NaN: the largest logit, the lowest index among equals, prob 1; top_k <= 0 or >= vocab, top_p >= 1 or NaN,
+ *   min_p <= 0 or NaN: off.  A logit of -inf or NaN is never taken; one of +inf is taken before all finite ones.  A row without any logit that
+ *   can be taken gives token -1, prob 0.  Tokens whose weight is below 2^-41 of the likeliest one's are not taken.
+ * status_dev is not written by this build.
+ */
+int gdn_sample(const gdn_sample_shape_t *shape, const void *logits, const float *temperature, const int32_t *top_k,
+               const float *top_p, const float *min_p, const float *uniform, int32_t *token, float *prob,
+               int32_t *status_dev, void *cuda_stream);
 
 #ifdef __cplusplus
 }

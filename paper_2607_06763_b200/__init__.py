@@ -6,7 +6,15 @@ library has not been built.
 """
 from . import synth  # noqa: F401
 from .binding import (  # noqa: F401
+    GdnAttnShape,
+    GdnSampleShape,
     GdnShape,
+    gdn_attn_decode,
+    gdn_attn_tree_verify,
+    gdn_attn_workspace_bytes,
+    gdn_kv_append,
+    gdn_kv_commit,
+    gdn_sample,
     gdn_status_string,
     gdn_tree_commit,
     gdn_tree_commit_host,

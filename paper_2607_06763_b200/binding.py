@@ -38,6 +38,12 @@ EXPORTS = (
     "gdn_tree_plan",
     "gdn_tree_verify_planned",
     "gdn_tree_commit_padded",
+    "gdn_attn_workspace_bytes",
+    "gdn_attn_decode",
+    "gdn_attn_tree_verify",
+    "gdn_kv_append",
+    "gdn_kv_commit",
+    "gdn_sample",
 )
 
 GDN_STATIC_SCRATCH_BYTES = 4 << 20
@@ -67,6 +73,71 @@ class GdnShape(ctypes.Structure):
         mt = int(sizes.max()) if len(sizes) else 1
         return cls(w.n_seq, w.h_qk, w.h_v, w.d_k, w.d_v, DTYPE_CODES[w.in_dtype], DTYPE_CODES[w.out_dtype],
                    max_depth, w.total_nodes, max(1, mt if max_tree_nodes is None else max_tree_nodes), w.scale)
+
+
+class GdnAttnShape(ctypes.Structure):
+    """Mirror of ``gdn_attn_shape_t``."""
+    _fields_ = [
+        ("n_seq", ctypes.c_int32),
+        ("h_q", ctypes.c_int32),
+        ("h_kv", ctypes.c_int32),
+        ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("total_rows", ctypes.c_int32),
+        ("max_rows", ctypes.c_int32),
+        ("n_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("max_len", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("page_stride", ctypes.c_int64),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+        ("q_stride", ctypes.c_int64),
+        ("k_stride", ctypes.c_int64),
+        ("v_stride", ctypes.c_int64),
+    ]
+
+    @classmethod
+    def from_cache(cls, k_cache, page_table, h_q: int, total_rows: int, max_rows: int, max_len: int | None = None,
+                   scale: float | None = None, q_stride: int | None = None, k_stride: int | None = None,
+                   v_stride: int | None = None) -> "GdnAttnShape":
+        """Shape of calls on a cache seen as ``[page][token][head][component]`` (any strides; the value cache has the same) with
+        ``page_table`` ``[n_seq][max_pages]``.  ``max_len`` defaults to all that a row of the table can hold, ``scale`` to
+        ``1/sqrt(d)``, the row strides to packed rows."""
+        n_pages, page_size, h_kv, d = k_cache.shape
+        if k_cache.stride(3) != 1:
+            raise ValueError("the components of a head must be contiguous")
+        dtype = {"torch.float32": GDN_F32, "torch.bfloat16": GDN_BF16}.get(str(k_cache.dtype))
+        if dtype is None:
+            raise ValueError(f"the cache is fp32 or bf16, not {k_cache.dtype}")
+        n_seq, max_pages = page_table.shape
+        return cls(n_seq, h_q, h_kv, d, dtype, total_rows, max_rows, n_pages, page_size, max_pages,
+                   max_pages * page_size if max_len is None else max(1, max_len), d ** -0.5 if scale is None else scale,
+                   k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), h_q * d if q_stride is None else q_stride,
+                   h_kv * d if k_stride is None else k_stride, h_kv * d if v_stride is None else v_stride)
+
+
+class GdnSampleShape(ctypes.Structure):
+    """Mirror of ``gdn_sample_shape_t``."""
+    _fields_ = [
+        ("n_rows", ctypes.c_int32),
+        ("vocab", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
+        ("row_stride", ctypes.c_int64),
+    ]
+
+    @classmethod
+    def from_logits(cls, logits) -> "GdnSampleShape":
+        """Shape of a sampling call on ``logits`` ``[rows][vocab]`` (rows may lie apart)."""
+        n_rows, vocab = logits.shape
+        if vocab > 1 and logits.stride(1) != 1:
+            raise ValueError("the logits of a row must be contiguous")
+        dtype = {"torch.float32": GDN_F32, "torch.bfloat16": GDN_BF16}.get(str(logits.dtype))
+        if dtype is None:
+            raise ValueError(f"logits are fp32 or bf16, not {logits.dtype}")
+        return cls(n_rows, vocab, dtype, 0, max(logits.stride(0), vocab) if n_rows <= 1 else logits.stride(0))
 
 
 def library_path() -> str:
@@ -125,6 +196,19 @@ def load_library():
         lib.gdn_tree_verify_static.argtypes = [sp] + [vp] * 11
         lib.gdn_tree_verify_recurrent.restype = ctypes.c_int
         lib.gdn_tree_verify_recurrent.argtypes = [sp] + [vp] * 11
+        ap, i32, sz = ctypes.POINTER(GdnAttnShape), ctypes.c_int32, ctypes.c_size_t
+        lib.gdn_attn_workspace_bytes.restype = sz
+        lib.gdn_attn_workspace_bytes.argtypes = [ap]
+        lib.gdn_attn_decode.restype = ctypes.c_int
+        lib.gdn_attn_decode.argtypes = [ap] + [vp] * 7 + [sz, vp, vp]
+        lib.gdn_attn_tree_verify.restype = ctypes.c_int
+        lib.gdn_attn_tree_verify.argtypes = [ap] + [vp] * 9 + [sz, vp, vp]
+        lib.gdn_kv_append.restype = ctypes.c_int
+        lib.gdn_kv_append.argtypes = [ap] + [vp] * 4 + [i32] * 3 + [vp] * 9
+        lib.gdn_kv_commit.restype = ctypes.c_int
+        lib.gdn_kv_commit.argtypes = [ap] + [vp] * 3 + [i32] * 3 + [vp] * 10
+        lib.gdn_sample.restype = ctypes.c_int
+        lib.gdn_sample.argtypes = [ctypes.POINTER(GdnSampleShape)] + [vp] * 10
         _lib = lib
     return _lib
 
@@ -154,10 +238,34 @@ def _call(address, *args) -> int:
     """Replaced by the C marshaller (``csrc/gdn_call.c``) on the first call; loading it here keeps the import of the
     package possible before the build."""
     global _call
-    from ._gdn_call import call, set_shape_type
-    set_shape_type(GdnShape)
+    _marshaller()
+    from ._gdn_call import call
     _call = call
     return call(address, *args)
+
+
+def _marshaller():
+    from ._gdn_call import set_shape_type, set_shape_types
+    set_shape_type(GdnShape)
+    set_shape_types(GdnAttnShape, GdnSampleShape)
+
+
+def _call_attn(address, *args) -> int:
+    """As ``_call``, for calls whose shape is a ``GdnAttnShape``."""
+    global _call_attn
+    _marshaller()
+    from ._gdn_call import call_attn
+    _call_attn = call_attn
+    return call_attn(address, *args)
+
+
+def _call_sample(address, *args) -> int:
+    """As ``_call``, for calls whose shape is a ``GdnSampleShape``."""
+    global _call_sample
+    _marshaller()
+    from ._gdn_call import call_sample
+    _call_sample = call_sample
+    return call_sample(address, *args)
 
 
 def _stream(stream):
@@ -280,3 +388,41 @@ def gdn_tree_commit_verify(shape: GdnShape, S, k_prev, v_prev, g_prev, beta_prev
     return _call(_entry["gdn_tree_commit_verify"], shape, S, k_prev, v_prev, g_prev, beta_prev, parent_prev,
                  node_offsets_prev, path, path_offsets, q, k, v, g, beta, parent, node_offsets, o, workspace,
                  int(workspace_bytes), status_dev, _stream(stream))
+
+
+def gdn_attn_workspace_bytes(shape: GdnAttnShape) -> int:
+    return int(load_library().gdn_attn_workspace_bytes(ctypes.byref(shape)))
+
+
+def gdn_kv_append(shape: GdnAttnShape, q, k, v, rope, rope_len, rope_dim, interleaved, parent, row_offsets, seq_lens, page_table, q_out,
+                  k_cache, v_cache, status_dev, stream=None) -> int:
+    """``gdn_kv_append``: new rows into a paged cache, keys (and queries, into ``q_out``) rotated by position."""
+    return _call_attn(_entry["gdn_kv_append"], shape, q, k, v, rope, int(rope_len), int(rope_dim), int(bool(interleaved)), parent,
+                      row_offsets, seq_lens, page_table, q_out, k_cache, v_cache, status_dev, _stream(stream))
+
+
+def gdn_kv_commit(shape: GdnAttnShape, k, v, rope, rope_len, rope_dim, interleaved, parent, row_offsets, path, path_offsets, seq_lens,
+                  page_table, k_cache, v_cache, status_dev, stream=None) -> int:
+    """``gdn_kv_commit``: the rows of accepted paths to the ends of their sequences in a paged cache."""
+    return _call_attn(_entry["gdn_kv_commit"], shape, k, v, rope, int(rope_len), int(rope_dim), int(bool(interleaved)), parent,
+                      row_offsets, path, path_offsets, seq_lens, page_table, k_cache, v_cache, status_dev, _stream(stream))
+
+
+def gdn_attn_decode(shape: GdnAttnShape, q, k_cache, v_cache, page_table, seq_lens, o, workspace, workspace_bytes, status_dev,
+                    stream=None) -> int:
+    """``gdn_attn_decode``: attention of one new token per sequence over its pages."""
+    return _call_attn(_entry["gdn_attn_decode"], shape, q, k_cache, v_cache, page_table, seq_lens, o, workspace, int(workspace_bytes),
+                      status_dev, _stream(stream))
+
+
+def gdn_attn_tree_verify(shape: GdnAttnShape, q, k_cache, v_cache, page_table, seq_lens, parent, row_offsets, o, workspace,
+                         workspace_bytes, status_dev, stream=None) -> int:
+    """``gdn_attn_tree_verify``: attention of the nodes of draft trees (or of prompt chunks, ``parent`` None) over pages."""
+    return _call_attn(_entry["gdn_attn_tree_verify"], shape, q, k_cache, v_cache, page_table, seq_lens, parent, row_offsets, o,
+                      workspace, int(workspace_bytes), status_dev, _stream(stream))
+
+
+def gdn_sample(shape: GdnSampleShape, logits, temperature, top_k, top_p, min_p, uniform, token, prob, status_dev, stream=None) -> int:
+    """``gdn_sample``: one token per row of logits by temperature, top-k, top-p and min-p, from given random numbers."""
+    return _call_sample(_entry["gdn_sample"], shape, logits, temperature, top_k, top_p, min_p, uniform, token, prob, status_dev,
+                        _stream(stream))

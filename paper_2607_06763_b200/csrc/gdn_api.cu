@@ -115,6 +115,7 @@ extern "C" const char *gdn_status_string(int status)
     case GDN_ERR_PATH: return "accepted path is not a root chain of its tree";
     case GDN_ERR_WORKSPACE: return "workspace missing or too small";
     case GDN_ERR_TIMEOUT: return "a bounded device-side wait expired";
+    case GDN_ERR_PAGE: return "a page id or a length lies outside the cache";
     default: return "unknown status";
     }
 }

@@ -1,0 +1,284 @@
+// What the attention kernels over a paged cache have in common: their arguments, how the work is cut up and handed out, which
+// cached token a row may see, and the places in the workspace.
+//
+// A unit is (sequence, key/value head, tile of M rows); row r of a unit is node r / G of the sequence's rows with query head
+// head * G + r % G (G = h_q / h_kv), so that the G query heads that share a key/value head share its tiles.  The tokens of a
+// unit come in tiles of TN.  Where a call has more than one tile per unit, the tiles of all units, one behind the other,
+// are cut into as many equal runs as there are CTAs: a batch of lengths from one to many thousands keeps every SM busy to the
+// end, whatever the lengths, which only the device knows.  A run that holds a whole unit writes its rows; the others leave
+// their unnormalised sums with maximum and denominator in the workspace, where the join kernel finds them by the same
+// arithmetic.  A CTA has at most two such parts: the first unit of its run, begun by another CTA, and the last.
+#pragma once
+
+#include "gdn_internal.cuh"
+#include "gdn_path.cuh"
+#include "gdn_tc.cuh"
+
+namespace gdn {
+
+constexpr int AT_SMALL_ROWS = 64;   // trees up to this size: every CTA derives the ancestors itself (one 64-bit word per node)
+
+struct AttnParams {
+    int n_seq, h_q, h_kv, group, d, total_rows, max_rows, n_pages, page_size, page_shift, max_pages, max_len;
+    float scale_log2;                                // scale * log2(e): scores in units of a power of two
+    long long page_stride, token_stride, head_stride, q_stride;   // in elements
+    const void *q, *k_cache, *v_cache;
+    const int32_t *page_table, *seq_lens, *row_offsets, *parent;  // row_offsets null: one row per sequence, all of its tokens seen
+    void *o;
+    int32_t *status_dev;
+    int split;                                       // 0: CTA = unit
+    int m_tiles;                                     // tiles of M rows that the longest sequence has
+    // workspace: ancestors of trees above AT_SMALL_ROWS nodes, then the parts of split units
+    uint32_t *mask;                                  // [total_rows][mask_words]
+    int mask_words;
+    int32_t *tree_ok;                                // [n_seq]
+    float *part_o, *part_ml;                         // [2 * CTAs][M][d], [2 * CTAs][M][2]
+    int n_ctas;
+};
+
+struct AttnLayout {
+    size_t mask, tree_ok, part_o, part_ml, total;
+};
+
+#ifdef __CUDACC__
+struct AttnSeq {
+    int len, rows, row0, held;   // committed tokens; rows of the call, the first of them; tokens that any row sees
+};
+
+// Lengths of sequence b; false where they are not possible (reported by the caller that is asked to).
+__device__ __forceinline__ bool attn_seq(const AttnParams &p, int b, AttnSeq &s, bool report)
+{
+    s.len = p.seq_lens[b];
+    if (p.row_offsets) {
+        const int r0 = p.row_offsets[b], r1 = p.row_offsets[b + 1];
+        s.row0 = r0;
+        s.rows = r1 - r0;
+        if (r0 < 0 || r1 > p.total_rows || r1 < r0 || s.rows > p.max_rows) {
+            if (report) report_status(p.status_dev, GDN_ERR_TREE);
+            return false;
+        }
+        if (s.len < 0 || s.len > p.max_len - s.rows) {
+            if (report) report_status(p.status_dev, GDN_ERR_PAGE);
+            return false;
+        }
+        s.held = s.len + s.rows;
+    } else {
+        s.row0 = b;
+        s.rows = 1;
+        s.held = s.len;
+        if (s.len < 0 || s.len > p.max_len) {
+            if (report) report_status(p.status_dev, GDN_ERR_PAGE);
+            return false;
+        }
+    }
+    return true;
+}
+
+struct AttnSegment {
+    AttnSeq s;
+    int b, head, m_tile;
+    int tile0, tile1, tiles;   // tiles [tile0, tile1) of the unit's `tiles`
+    int slot;                  // place of the part in the workspace, -1: the whole unit
+};
+
+__device__ __forceinline__ int attn_tiles(const AttnSeq &s, int TN) { return s.held > TN ? (s.held + TN - 1) / TN : 1; }
+
+__device__ __forceinline__ long long attn_seq_work(const AttnParams &p, int b, int M, int TN, AttnSeq &s, bool report)
+{
+    if (!attn_seq(p, b, s, report)) return 0;
+    return (long long)p.h_kv * ((s.rows * p.group + M - 1) / M) * attn_tiles(s, TN);
+}
+
+// Sum over the lanes up to and including this one.
+__device__ __forceinline__ long long warp_scan(long long x, int lane)
+{
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const long long up = __shfl_up_sync(0xffffffffu, x, off);
+        if (lane >= off) x += up;
+    }
+    return x;
+}
+
+// The run of one CTA, walked by every warp on its own (the same values in all of them; no exchange between warps).
+struct AttnWalk {
+    long long at, end;   // tiles of the run, counted over all units
+    long long seq_at;    // the first tile of sequence b
+    int b;
+    AttnSeq s;
+
+    __device__ __forceinline__ void begin(const AttnParams &p, int cta, int M, int TN)
+    {
+        if (!p.split) {   // CTA = unit, the last rows (the most tokens) first
+            at = 0;
+            end = 1;
+            return;
+        }
+        const int lane = threadIdx.x & 31;
+        const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
+        long long mine = 0;
+        for (int i = b0; i < b1; ++i) {
+            AttnSeq t;
+            mine += attn_seq_work(p, i, M, TN, t, cta == 0 && threadIdx.x < 32);
+        }
+        const long long upto = warp_scan(mine, lane), total = __shfl_sync(0xffffffffu, upto, 31);
+        const long long runs = total < p.n_ctas ? total : p.n_ctas;
+        at = end = 0;
+        if (cta >= runs) return;
+        at = total * cta / runs;
+        end = total * (cta + 1) / runs;
+        // the lane whose sequences hold tile `at` looks for it among them
+        const unsigned holds = __ballot_sync(0xffffffffu, upto > at);
+        const int owner = __ffs(holds) - 1;
+        int found = 0;
+        long long begins = upto - mine;
+        if (lane == owner)
+            for (int i = b0; i < b1; ++i) {
+                AttnSeq t;
+                const long long w = attn_seq_work(p, i, M, TN, t, false);
+                if (begins + w > at) {
+                    found = i;
+                    break;
+                }
+                begins += w;
+            }
+        b = __shfl_sync(0xffffffffu, found, owner);
+        seq_at = __shfl_sync(0xffffffffu, begins, owner);
+    }
+
+    __device__ __forceinline__ bool next(const AttnParams &p, int cta, int M, int TN, AttnSegment &g)
+    {
+        if (at >= end) return false;
+        if (!p.split) {
+            at = end;
+            const int per_seq = p.h_kv * p.m_tiles;
+            g.b = cta / per_seq;
+            g.m_tile = p.m_tiles - 1 - cta % per_seq / p.h_kv;
+            g.head = cta % p.h_kv;
+            g.tile0 = 0;
+            g.slot = -1;
+            if (!attn_seq(p, g.b, g.s, g.head == 0 && g.m_tile == 0) || g.m_tile * M >= g.s.rows * p.group) return false;
+            g.tile1 = g.tiles = attn_tiles(g.s, TN);
+            return true;
+        }
+        for (;;) {   // ends: tile `at` of the `total` belongs to some sequence
+            const long long w = attn_seq_work(p, b, M, TN, s, false);
+            if (at < seq_at + w) break;
+            seq_at += w;
+            ++b;
+        }
+        g.s = s;
+        g.b = b;
+        g.tiles = attn_tiles(s, TN);
+        const int unit = (int)((at - seq_at) / g.tiles);
+        const int m_tiles = (s.rows * p.group + M - 1) / M;
+        g.head = unit / m_tiles;
+        g.m_tile = unit % m_tiles;
+        g.tile0 = (int)((at - seq_at) - (long long)unit * g.tiles);
+        const long long left = end - at;
+        g.tile1 = left < g.tiles - g.tile0 ? g.tile0 + (int)left : g.tiles;
+        g.slot = g.tile0 == 0 ? (g.tile1 == g.tiles ? -1 : 2 * cta + 1) : 2 * cta;
+        at += g.tile1 - g.tile0;
+        return true;
+    }
+};
+
+// Where token t of sequence b lies in the cache, in elements from its base for head 0; -1 where the page table says nothing
+// possible (reported) or t is behind the last token.
+__device__ __forceinline__ long long attn_token_offset(const AttnParams &p, int b, int t, int held)
+{
+    if (t >= held) return -1;
+    const int entry = p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size;
+    const int page = p.page_table[(size_t)b * p.max_pages + entry];
+    if (page < 0 || page >= p.n_pages) {
+        report_status(p.status_dev, GDN_ERR_PAGE);
+        return -1;
+    }
+    return page * p.page_stride + (t - entry * p.page_size) * p.token_stride;
+}
+
+// Ancestors of the nodes of a tree of at most 64 nodes, the node itself among them, by all threads of the CTA (at least 64);
+// a and up are [64] each.  False where the tree is none.  Doubling: after k rounds a node knows its next 2^k ancestors.
+__device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSeq &s, unsigned long long *a, int *up)
+{
+    const int i = threadIdx.x;
+    int parent = -1;
+    bool bad = false;
+    if (i < s.rows) {
+        parent = p.parent[s.row0 + i];
+        bad = parent < -1 || parent >= i;
+    }
+    if (__syncthreads_or(bad)) return false;
+    if (i < AT_SMALL_ROWS) {
+        a[i] = 1ull << i;
+        up[i] = parent;
+    }
+    __syncthreads();
+    for (int step = 1; step < s.rows; step <<= 1) {
+        unsigned long long mine = 0;
+        int next = -1;
+        if (i < AT_SMALL_ROWS) {
+            mine = a[i];
+            next = up[i];
+            if (next >= 0) {
+                mine |= a[next];
+                next = up[next];
+            }
+        }
+        __syncthreads();
+        if (i < AT_SMALL_ROWS) {
+            a[i] = mine;
+            up[i] = next;
+        }
+        __syncthreads();
+    }
+    return true;
+}
+
+// Whether row node i sees node j of its sequence's rows (i, j < rows).
+enum AttnMaskKind { AT_CHAIN, AT_WORDS64, AT_WORDS };
+__device__ __forceinline__ bool attn_sees(const AttnParams &p, AttnMaskKind kind, const unsigned long long *a, int row0, int i, int j)
+{
+    if (j > i) return false;
+    if (kind == AT_CHAIN) return true;
+    if (kind == AT_WORDS64) return a[i] >> j & 1;
+    return p.mask[(size_t)(row0 + i) * p.mask_words + (j >> 5)] >> (j & 31) & 1;
+}
+__device__ __forceinline__ AttnMaskKind attn_mask_kind(const AttnParams &p)
+{
+    return !p.parent ? AT_CHAIN : p.max_rows <= AT_SMALL_ROWS ? AT_WORDS64 : AT_WORDS;
+}
+#endif
+
+constexpr int AT_SMS = 148;
+struct AttnTiling {
+    int M, TN, ctas;   // rows and tokens of a tile, CTAs that an SM holds
+};
+AttnTiling attn_general_tiling();
+// `bf16`: the type of rows, cache and outputs; otherwise fp32.
+cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream);
+cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream);
+cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream);
+
+cudaError_t launch_kv_append(const AttnParams &a, bool bf16, const void *k, const void *v, long long k_stride, long long v_stride,
+                             const float *rope, int rope_dim, bool interleaved, void *q_out, void *k_out, void *v_out,
+                             const int32_t *path, const int32_t *path_offsets, cudaStream_t stream);
+
+// A launch that may become resident under the tail of the kernel in front of it, where it waits (wait_for_previous_kernel).
+template <typename... KernelArgs, typename... Args>
+cudaError_t launch_behind(void (*kernel)(KernelArgs...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace gdn

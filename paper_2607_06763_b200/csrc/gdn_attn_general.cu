@@ -1,0 +1,314 @@
+// Attention over a paged cache on CUDA cores: any head size, fp32 or bf16; and what every kernel of the family uses: the
+// ancestors of large trees, the join of parts.
+//
+// For row i and the tokens t that it sees, with s_t = scale * q_i . k_t:
+//     o_i = sum_t 2^(s'_t - m) v_t / sum_t 2^(s'_t - m),   s' = s * log2(e),  m = max_t s'_t,
+// in one pass over the tokens: where a tile raises the maximum from m to m', what has been summed so far is multiplied
+// by 2^(m - m').  A row that sees nothing has the sum 0 and the output 0.
+#include "gdn_attn.cuh"
+
+namespace gdn {
+
+namespace {
+
+constexpr int AG_THREADS = 128;
+constexpr int AG_M = 16;       // rows of a unit: four per warp
+constexpr int AG_TN = 32;      // tokens of a tile: one per lane
+constexpr int AG_STAGES = 2;
+
+template <typename T> __host__ __device__ constexpr int ag_pitch(int d) { return d * (int)sizeof(T) + 16; }   // the next row begins four banks on
+template <typename T> constexpr size_t ag_smem(int d)
+{
+    return (size_t)AG_STAGES * 2 * AG_TN * ag_pitch<T>(d) + AG_M * d * sizeof(float) + AG_M * AG_TN * sizeof(float);
+}
+
+__device__ __forceinline__ float4 four(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+__device__ __forceinline__ float4 four(const __nv_bfloat16 *p)
+{
+    const uint2 u = *reinterpret_cast<const uint2 *>(p);
+    return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xFFFF0000u), __uint_as_float(u.y << 16),
+                       __uint_as_float(u.y & 0xFFFF0000u));
+}
+
+// Four warps, each with four rows; a lane has a token in the products with the keys and four components in those with the
+// values.  Bound by shared memory for many rows (a key's four components feed sixteen multiplications), by HBM for few.
+template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general_kernel(const AttnParams p)
+{
+    extern __shared__ __align__(16) unsigned char ag_smem_base[];
+    __shared__ unsigned long long anc[AT_SMALL_ROWS];
+    __shared__ int anc_up[AT_SMALL_ROWS];
+    const int d = p.d, pitch = ag_pitch<T>(d), stage_bytes = 2 * AG_TN * pitch;
+    float *q_s = reinterpret_cast<float *>(ag_smem_base + AG_STAGES * stage_bytes);
+    float *w_s = q_s + AG_M * d;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = (int)blockIdx.x;
+    const AttnMaskKind kind = attn_mask_kind(p);
+    const T *k_cache = static_cast<const T *>(p.k_cache), *v_cache = static_cast<const T *>(p.v_cache);
+    wait_for_previous_kernel();
+
+    AttnWalk walk;
+    AttnSegment g;
+    walk.begin(p, cta, AG_M, AG_TN);
+    while (walk.next(p, cta, AG_M, AG_TN, g)) {
+        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up)) {
+            if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
+            continue;
+        }
+        if (p.row_offsets && kind == AT_WORDS && !p.tree_ok[g.b]) continue;
+        const int row_first = g.m_tile * AG_M, rows = min(AG_M, g.s.rows * p.group - row_first);
+        for (int i = tid; i < rows * d; i += AG_THREADS) {
+            const int r = (row_first + i / d), node = r / p.group;
+            q_s[i] = load_as_float(static_cast<const T *>(p.q) + (size_t)(g.s.row0 + node) * p.q_stride +
+                                   (size_t)(g.head * p.group + r % p.group) * d + i % d);
+        }
+        // the last token that any of these rows sees: rows come in an order in which ancestors are in front
+        const int last_node = (row_first + rows - 1) / p.group, upto = p.row_offsets ? g.s.len + last_node + 1 : g.s.len;
+        const int tile1 = min(g.tile1, max((upto + AG_TN - 1) / AG_TN, g.tile0));
+
+        auto fetch = [&](int tile) {   // rows warp * 8 ... + 7 of the keys and of the values
+            if (tile < tile1) {
+                const uint32_t base = smem_u32(ag_smem_base) + (tile % AG_STAGES) * stage_bytes;
+                const long long mine = attn_token_offset(p, g.b, tile * AG_TN + lane, min(g.s.held, upto));
+                for (int r = warp * 8; r < warp * 8 + 8; ++r) {
+                    const long long at = __shfl_sync(0xffffffffu, mine, r);
+                    const long long from = (at < 0 ? 0 : at) + (long long)g.head * p.head_stride;
+                    if (lane * 16 < d * (int)sizeof(T)) {
+                        cp_async_16(base + r * pitch + lane * 16, reinterpret_cast<const char *>(k_cache + from) + lane * 16, at >= 0);
+                        cp_async_16(base + (AG_TN + r) * pitch + lane * 16, reinterpret_cast<const char *>(v_cache + from) + lane * 16,
+                                    at >= 0);
+                    }
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+
+        float m[4], l[4], acc[4][4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[r][c] = 0.f;
+        }
+        fetch(g.tile0);
+        for (int tile = g.tile0; tile < tile1; ++tile) {
+            fetch(tile + 1);
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncthreads();
+            if (warp * 4 < rows) {
+                const T *k_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + lane * pitch);
+                float sc[4] = {0.f, 0.f, 0.f, 0.f};
+                const float *qw = q_s + warp * 4 * d;
+#pragma unroll 4
+                for (int c = 0; c < d; c += 4) {
+                    const float4 k4 = four(k_s + c);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float4 q4 = four(qw + r * d + c);
+                        sc[r] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, sc[r]))));
+                    }
+                }
+                const int t = tile * AG_TN + lane;
+                float4 w;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int row = warp * 4 + r, node = (row_first + row) / p.group;
+                    const bool seen = row < rows && (t < g.s.len || (t < g.s.held && attn_sees(p, kind, anc, g.s.row0, node, t - g.s.len)));
+                    const float x = seen ? sc[r] * p.scale_log2 : -INFINITY;
+                    float top = x;
+#pragma unroll
+                    for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+                    top = fmaxf(top, m[r]);
+                    const float ref = top == -INFINITY ? 0.f : top;
+                    const float e = seen ? exp2f(x - ref) : 0.f, fade = exp2f(m[r] - ref);
+                    m[r] = top;
+                    float sum = e;
+#pragma unroll
+                    for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                    l[r] = l[r] * fade + sum;
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[r][c] *= fade;
+                    (&w.x)[r] = e;
+                }
+                reinterpret_cast<float4 *>(w_s)[warp * AG_TN + lane] = w;
+                __syncwarp();
+                if (lane * 4 < d) {
+                    const T *v_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + AG_TN * pitch) + lane * 4;
+#pragma unroll 8
+                    for (int j = 0; j < AG_TN; ++j) {
+                        const float4 e = reinterpret_cast<const float4 *>(w_s)[warp * AG_TN + j];
+                        const float4 v4 = four(reinterpret_cast<const T *>(reinterpret_cast<const char *>(v_s) + j * pitch));
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float er = (&e.x)[r];
+                            if (er != 0.f) {   // (a value that a row does not see may be infinite or no number)
+                                acc[r][0] = fmaf(er, v4.x, acc[r][0]);
+                                acc[r][1] = fmaf(er, v4.y, acc[r][1]);
+                                acc[r][2] = fmaf(er, v4.z, acc[r][2]);
+                                acc[r][3] = fmaf(er, v4.w, acc[r][3]);
+                            }
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int row = warp * 4 + r;
+            if (row >= rows) continue;
+            if (g.slot < 0) {
+                if (lane * 4 < d) {
+                    const int u = row_first + row;
+                    T *o = static_cast<T *>(p.o) + ((size_t)(g.s.row0 + u / p.group) * p.h_q + g.head * p.group + u % p.group) * d + lane * 4;
+                    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) store_from_float(o + c, acc[r][c] * inv);
+                }
+            } else {
+                const size_t at = (size_t)g.slot * AG_M + row;
+                if (lane * 4 < d) *reinterpret_cast<float4 *>(p.part_o + at * d + lane * 4) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+                if (lane == 0) *reinterpret_cast<float2 *>(p.part_ml + at * 2) = make_float2(m[r], l[r]);
+            }
+        }
+        __syncthreads();   // (the next unit's queries and ancestors)
+    }
+}
+
+// Ancestors of the nodes of trees above AT_SMALL_ROWS nodes, as a bit per node of the tree: row i of `mask` holds the words up
+// to that of node i itself.  A thread walks its node's root path; ids fall along it, so that every word is written once.
+constexpr int AM_THREADS = 256;
+__global__ void __launch_bounds__(AM_THREADS) attn_mask_kernel(const AttnParams p)
+{
+    extern __shared__ int am_parent[];
+    wait_for_previous_kernel();
+    const int b = (int)blockIdx.y, first = (int)blockIdx.x * AM_THREADS;
+    AttnSeq s;
+    const bool fits = attn_seq(p, b, s, false);
+    if (!fits || (first > 0 && first >= s.rows)) return;   // (first = 0: an empty tree is one)
+    bool bad = false;
+    for (int i = threadIdx.x; i < s.rows; i += AM_THREADS) {
+        const int parent = p.parent[s.row0 + i];
+        am_parent[i] = parent;
+        bad |= parent < -1 || parent >= i;
+    }
+    bad = __syncthreads_or(bad);
+    if (first == 0 && threadIdx.x == 0) {
+        p.tree_ok[b] = !bad;
+        if (bad) report_status(p.status_dev, GDN_ERR_TREE);
+    }
+    const int i = first + (int)threadIdx.x;
+    if (bad || i >= s.rows) return;
+    int node = i;
+    for (int w = i >> 5; w >= 0; --w) {
+        uint32_t bits = 0;
+        while (node >= 0 && node >> 5 == w) {
+            bits |= 1u << (node & 31);
+            node = am_parent[node];
+        }
+        p.mask[(size_t)(s.row0 + i) * p.mask_words + w] = bits;
+    }
+}
+
+// The parts of a split unit, in the order of their tiles, to its rows: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
+// One warp per row, the CTAs of a unit eight rows each; a unit that one run held is left alone.
+constexpr int AJ_THREADS = 256;
+template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_kernel(const AttnParams p, int M, int TN)
+{
+    wait_for_previous_kernel();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int units = p.h_kv * p.m_tiles, b = (int)blockIdx.x / units, head = (int)blockIdx.x % units / p.m_tiles, m_tile = (int)blockIdx.x % p.m_tiles;
+    AttnSeq s;
+    if (!attn_seq(p, b, s, false)) return;
+    const int row_first = m_tile * M, row = (int)blockIdx.y * 8 + warp, rows = min(M, s.rows * p.group - row_first);
+    if ((int)blockIdx.y * 8 >= rows) return;
+    if (p.row_offsets && p.parent) {
+        if (p.max_rows > AT_SMALL_ROWS) {
+            if (!p.tree_ok[b]) return;
+        } else {
+            bool bad = false;
+            if ((int)threadIdx.x < s.rows) {
+                const int parent = p.parent[s.row0 + threadIdx.x];
+                bad = parent < -1 || parent >= (int)threadIdx.x;
+            }
+            if (__syncthreads_or(bad)) return;
+        }
+    }
+    // the first tile of this unit among those of all units, as AttnWalk counts them
+    const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
+    long long mine = 0, before = 0;
+    for (int i = b0; i < b1; ++i) {
+        AttnSeq t;
+        const long long w = attn_seq_work(p, i, M, TN, t, false);
+        mine += w;
+        if (i < b) before += w;
+    }
+    long long total = mine;
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, off);
+        before += __shfl_xor_sync(0xffffffffu, before, off);
+    }
+    const int tiles = attn_tiles(s, TN), m_tiles = (s.rows * p.group + M - 1) / M;
+    const long long first = before + (long long)(head * m_tiles + m_tile) * tiles, last = first + tiles - 1;
+    const long long runs = total < p.n_ctas ? total : p.n_ctas;
+    const int c0 = (int)(((first + 1) * runs - 1) / total), c1 = (int)(((last + 1) * runs - 1) / total);
+    if (c0 == c1 || row >= rows) return;
+
+    float m = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, p.part_ml[((size_t)(c == c0 ? 2 * c + 1 : 2 * c) * M + row) * 2]);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+        const size_t at = (size_t)(c == c0 ? 2 * c + 1 : 2 * c) * M + row;
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + at * 2);
+        const float f = exp2f(ml.x - ref);
+        l = fmaf(f, ml.y, l);
+        if (lane * 4 < p.d && ml.x != -INFINITY) {
+            const float4 v = *reinterpret_cast<const float4 *>(p.part_o + at * p.d + lane * 4);
+            acc[0] = fmaf(f, v.x, acc[0]);
+            acc[1] = fmaf(f, v.y, acc[1]);
+            acc[2] = fmaf(f, v.z, acc[2]);
+            acc[3] = fmaf(f, v.w, acc[3]);
+        }
+    }
+    if (lane * 4 < p.d) {
+        const int u = row_first + row;
+        T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + lane * 4;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) store_from_float(o + c, acc[c] * inv);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream)
+{
+    return launch_behind(attn_mask_kernel, dim3((unsigned)((p.max_rows + AM_THREADS - 1) / AM_THREADS), (unsigned)p.n_seq), AM_THREADS,
+                         (size_t)p.max_rows * sizeof(int), stream, p);
+}
+
+cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream)
+{
+    const dim3 grid((unsigned)(p.n_seq * p.h_kv * p.m_tiles), (unsigned)((min(M, p.max_rows * p.group) + 7) / 8));
+    return bf16 ? launch_behind(attn_join_kernel<__nv_bfloat16>, grid, AJ_THREADS, 0, stream, p, M, TN)
+                : launch_behind(attn_join_kernel<float>, grid, AJ_THREADS, 0, stream, p, M, TN);
+}
+
+AttnTiling attn_general_tiling() { return {AG_M, AG_TN, 3}; }
+
+cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream)
+{
+    static PerContext seen[2];
+    const auto kernel = bf16 ? attn_general_kernel<__nv_bfloat16> : attn_general_kernel<float>;
+    int sms = 0;
+    const cudaError_t e = device_sms(seen[bf16], reinterpret_cast<const void *>(kernel), bf16 ? ag_smem<__nv_bfloat16>(GDN_MAX_HEAD_DIM) : ag_smem<float>(GDN_MAX_HEAD_DIM), &sms);
+    if (e != cudaSuccess) return e;
+    return launch_behind(kernel, dim3((unsigned)grid), AG_THREADS, bf16 ? ag_smem<__nv_bfloat16>(p.d) : ag_smem<float>(p.d), stream, p);
+}
+
+}  // namespace gdn

@@ -9,7 +9,8 @@
 
 enum { MAX_ARGS = 24 };
 static PyObject *s_data_ptr, *s_ctypes, *s_data;
-static PyObject *shape_type;   /* GdnShape, a ctypes.Structure */
+static PyObject *shape_type;   /* GdnShape, a ctypes.Structure; of the calls over a cache and of the sampler: set_shape_types */
+static PyObject *attn_type, *sample_type;
 
 static int value_of(PyObject *x, uint64_t *out)
 {
@@ -17,13 +18,13 @@ static int value_of(PyObject *x, uint64_t *out)
     return *out == (uint64_t)-1 && PyErr_Occurred() ? -1 : 0;
 }
 
-static int shape_of(PyObject *x, uint64_t *out)
+static int shape_of(PyObject *x, PyObject *type, const char *name, uint64_t *out)
 {
     Py_buffer view;
-    const int is_shape = shape_type ? PyObject_IsInstance(x, shape_type) : 0;
+    const int is_shape = type ? PyObject_IsInstance(x, type) : 0;
     if (is_shape < 0) return -1;
     if (!is_shape) {
-        PyErr_Format(PyExc_TypeError, "the shape is a GdnShape, not %R", (PyObject *)Py_TYPE(x));
+        PyErr_Format(PyExc_TypeError, "the shape is a %s, not %R", name, (PyObject *)Py_TYPE(x));
         return -1;
     }
     if (PyObject_GetBuffer(x, &view, PyBUF_STRIDED_RO) != 0) return -1;
@@ -63,23 +64,52 @@ typedef int (*abi_fn)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t
                       uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, uint64_t,
                       uint64_t, uint64_t, uint64_t, uint64_t);
 
-static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
+static PyObject *call_with(PyObject *type, const char *name, PyObject *const *args, Py_ssize_t n)
 {
     uint64_t a[MAX_ARGS + 1] = {0};
     int rc;
-    (void)self;
     if (n < 2 || n > MAX_ARGS + 1) {
         PyErr_SetString(PyExc_TypeError, "call(address, shape, up to 23 arguments)");
         return NULL;
     }
     for (Py_ssize_t i = 0; i < n; ++i)
-        if ((i == 1 ? shape_of(args[i], &a[i]) : address_of(args[i], &a[i])) != 0) return NULL;
+        if ((i == 1 ? shape_of(args[i], type, name, &a[i]) : address_of(args[i], &a[i])) != 0) return NULL;
     /* the *_host entry points synchronise: other Python threads run meanwhile, as they do under ctypes */
     Py_BEGIN_ALLOW_THREADS
     rc = ((abi_fn)(uintptr_t)a[0])(a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14],
                                    a[15], a[16], a[17], a[18], a[19], a[20], a[21], a[22], a[23], a[24]);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
+}
+
+static PyObject *call(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    return call_with(shape_type, "GdnShape", args, n);
+}
+
+static PyObject *call_attn(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    return call_with(attn_type, "GdnAttnShape", args, n);
+}
+
+static PyObject *call_sample(PyObject *self, PyObject *const *args, Py_ssize_t n)
+{
+    (void)self;
+    return call_with(sample_type, "GdnSampleShape", args, n);
+}
+
+static PyObject *set_shape_types(PyObject *self, PyObject *args)
+{
+    PyObject *attn, *sample;
+    (void)self;
+    if (!PyArg_ParseTuple(args, "OO", &attn, &sample)) return NULL;
+    Py_INCREF(attn);
+    Py_XSETREF(attn_type, attn);
+    Py_INCREF(sample);
+    Py_XSETREF(sample_type, sample);
+    Py_RETURN_NONE;
 }
 
 static PyObject *set_shape_type(PyObject *self, PyObject *type)
@@ -91,7 +121,10 @@ static PyObject *set_shape_type(PyObject *self, PyObject *type)
 }
 
 static PyMethodDef methods[] = {{"call", (PyCFunction)(void (*)(void))call, METH_FASTCALL, NULL},
+                                {"call_attn", (PyCFunction)(void (*)(void))call_attn, METH_FASTCALL, NULL},
+                                {"call_sample", (PyCFunction)(void (*)(void))call_sample, METH_FASTCALL, NULL},
                                 {"set_shape_type", set_shape_type, METH_O, NULL},
+                                {"set_shape_types", set_shape_types, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_gdn_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
