@@ -41,6 +41,14 @@ struct AttnLayout {
 };
 
 #ifdef __CUDACC__
+// 2^x to 2^-22 of itself (0 for -inf).
+__device__ __forceinline__ float power_of_two(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 struct AttnSeq {
     int len, rows, row0, held;   // committed tokens; rows of the call, the first of them; tokens that any row sees
 };
@@ -257,6 +265,9 @@ struct AttnTiling {
 AttnTiling attn_general_tiling();
 // `bf16`: the type of rows, cache and outputs; otherwise fp32.
 cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream);
+// bf16, d = 64 or 128, tiles of 16, 32 or 64 rows.
+AttnTiling attn_rows_tiling(int rows, int d);
+cudaError_t launch_attn_rows(const AttnParams &p, int M, int grid, cudaStream_t stream);
 cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream);
 cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream);
 

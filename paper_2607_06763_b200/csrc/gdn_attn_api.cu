@@ -34,15 +34,16 @@ int check_attn_shape(const gdn_attn_shape_t *s)
 struct Choice {
     AttnTiling tiling;
     int m_tiles, grid;
-    bool split;
+    bool split, general;
     AttnLayout layout;
 };
 
 // The kernel for a shape, its grid, and the places in the workspace; false: more units than a grid has CTAs.
 bool choose(const gdn_attn_shape_t &s, Choice &c)
 {
-    c.tiling = attn_general_tiling();
     const long long rows = (long long)s.max_rows * (s.h_q / s.h_kv);
+    c.general = !(s.dtype == GDN_BF16 && (s.d == 64 || s.d == 128));
+    c.tiling = c.general ? attn_general_tiling() : attn_rows_tiling((int)rows, s.d);
     c.m_tiles = (int)((rows + c.tiling.M - 1) / c.tiling.M);
     const long long units = (long long)s.n_seq * s.h_kv * c.m_tiles, tiles = ((long long)s.max_len + c.tiling.TN - 1) / c.tiling.TN;
     if (units > 0x7fffffffLL) return false;
@@ -117,7 +118,8 @@ int attention(const gdn_attn_shape_t *shape, const void *q, const void *k_cache,
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = s.dtype == GDN_BF16;
     if (parent && s.max_rows > AT_SMALL_ROWS && launch_attn_masks(p, stream) != cudaSuccess) return GDN_ERR_CUDA;
-    if (launch_attn_general(p, bf16, c.grid, stream) != cudaSuccess) return GDN_ERR_CUDA;
+    if ((c.general ? launch_attn_general(p, bf16, c.grid, stream) : launch_attn_rows(p, c.tiling.M, c.grid, stream)) != cudaSuccess)
+        return GDN_ERR_CUDA;
     if (c.split && launch_attn_join(p, bf16, c.tiling.M, c.tiling.TN, stream) != cudaSuccess) return GDN_ERR_CUDA;
     return GDN_OK;
 }
