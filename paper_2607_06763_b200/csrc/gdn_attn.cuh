@@ -268,6 +268,9 @@ cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaSt
 // bf16, d = 64 or 128, tiles of 16, 32 or 64 rows.
 AttnTiling attn_rows_tiling(int rows, int d);
 cudaError_t launch_attn_rows(const AttnParams &p, int M, int grid, cudaStream_t stream);
+// bf16, d = 64 or 128, scale > 0, tiles of 256 rows.
+AttnTiling attn_sm100_tiling();
+cudaError_t launch_attn_sm100(const AttnParams &p, int grid, cudaStream_t stream);
 cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream);
 cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream);
 

@@ -34,7 +34,8 @@ int check_attn_shape(const gdn_attn_shape_t *s)
 struct Choice {
     AttnTiling tiling;
     int m_tiles, grid;
-    bool split, general;
+    bool split;
+    enum { GENERAL, ROWS, SM100 } kernel;
     AttnLayout layout;
 };
 
@@ -42,13 +43,16 @@ struct Choice {
 bool choose(const gdn_attn_shape_t &s, Choice &c)
 {
     const long long rows = (long long)s.max_rows * (s.h_q / s.h_kv);
-    c.general = !(s.dtype == GDN_BF16 && (s.d == 64 || s.d == 128));
-    c.tiling = c.general ? attn_general_tiling() : attn_rows_tiling((int)rows, s.d);
+    // up to 64 rows per key/value head the keys and values decide, and one tile of rows reads them once; above, the products do.
+    // (The kernel of the latter takes maxima of unscaled scores: a scale that turns or hides their order is the other's.)
+    c.kernel = !(s.dtype == GDN_BF16 && (s.d == 64 || s.d == 128)) ? Choice::GENERAL : rows <= 64 || !(s.scale > 0.f) ? Choice::ROWS : Choice::SM100;
+    c.tiling = c.kernel == Choice::GENERAL ? attn_general_tiling() : c.kernel == Choice::ROWS ? attn_rows_tiling((int)rows, s.d) : attn_sm100_tiling();
     c.m_tiles = (int)((rows + c.tiling.M - 1) / c.tiling.M);
     const long long units = (long long)s.n_seq * s.h_kv * c.m_tiles, tiles = ((long long)s.max_len + c.tiling.TN - 1) / c.tiling.TN;
     if (units > 0x7fffffffLL) return false;
-    c.split = tiles > 1;
     const long long resident = (long long)c.tiling.ctas * AT_SMS;
+    // a chunk of a prompt with more units than two for every CTA goes without: its units see ever more tokens, and the longest begin first
+    c.split = tiles > 1 && !(c.m_tiles > 1 && units >= 2 * resident);
     c.grid = (int)(!c.split ? units : units * tiles < resident ? units * tiles : resident);
     size_t off = 0;
     auto take = [&](size_t bytes) {
@@ -118,8 +122,10 @@ int attention(const gdn_attn_shape_t *shape, const void *q, const void *k_cache,
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = s.dtype == GDN_BF16;
     if (parent && s.max_rows > AT_SMALL_ROWS && launch_attn_masks(p, stream) != cudaSuccess) return GDN_ERR_CUDA;
-    if ((c.general ? launch_attn_general(p, bf16, c.grid, stream) : launch_attn_rows(p, c.tiling.M, c.grid, stream)) != cudaSuccess)
-        return GDN_ERR_CUDA;
+    const cudaError_t e = c.kernel == Choice::GENERAL ? launch_attn_general(p, bf16, c.grid, stream)
+                          : c.kernel == Choice::ROWS  ? launch_attn_rows(p, c.tiling.M, c.grid, stream)
+                                                      : launch_attn_sm100(p, c.grid, stream);
+    if (e != cudaSuccess) return GDN_ERR_CUDA;
     if (c.split && launch_attn_join(p, bf16, c.tiling.M, c.tiling.TN, stream) != cudaSuccess) return GDN_ERR_CUDA;
     return GDN_OK;
 }
