@@ -9,9 +9,11 @@
 // overwrites S in tensor memory (128 columns of S and D of O per stream).  Maxima that rise by less than 2^8 do not move the sums:
 // weights up to 256 are as exact in bf16, and O is multiplied only where a row's maximum has risen by more.
 //
-// Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values (cp.async, so that pages of any
-// size and stride do, into the swizzled layout of the products' operands), warp 11 the queries, warp 10 the products.  Two stages of
-// keys and of values, each with its own barriers.
+// Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, warp 10 the products.
+// Two stages of keys and of values, each with its own barriers.  Pages of 8 tokens or more, in powers of two, come by tensor copies, a
+// page or a part of one each, straight into the swizzled layout of the products' operands; others by cp.async, row by row: one warp needs
+// 3300 clocks to issue a tile that way, the products of two streams 2048.
+// A row's 128 scores stay in its thread's registers (the warps of the rows take over what the others leave).
 // Every wait is bounded; one that expires raises a flag that ends the others.
 #include "gdn_attn.cuh"
 
@@ -29,7 +31,7 @@ template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t
 struct SplitShared {
     unsigned long long anc[AT_SMALL_ROWS];
     int anc_up[AT_SMALL_ROWS];
-    unsigned long long q_full, k_full[AS_STAGES], v_full[AS_STAGES], k_empty[AS_STAGES], v_empty[AS_STAGES], s_full[2], p_full[2], o_full[2];
+    unsigned long long q_full, k_full[AS_STAGES], v_full[AS_STAGES], v_landed[AS_STAGES], k_empty[AS_STAGES], v_empty[AS_STAGES], s_full[2], p_full[2], o_full[2];
     uint32_t tmem;
     int odd, dead;
 };
@@ -86,7 +88,39 @@ __device__ __forceinline__ uint32_t seen_word(const AttnParams &p, AttnMaskKind 
     return __funnelshift_r(lo, hi, first & 31);
 }
 
-template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_kernel(const AttnParams p)
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm, int x, int y, int z, int w, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+
+struct CacheMaps {
+    CUtensorMap k, v;   // [page][head][token][component], boxes of 64 components of `box` tokens
+    int box;
+};
+
+// Makes what is infinite or no number in eight bf16 values zero; whether there was any.
+__device__ __forceinline__ bool zero_odd(uint4 &u)
+{
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t &y = (&u.x)[e];
+        if ((y & 0x7F80u) == 0x7F80u) { y &= 0xFFFF0000u; odd = true; }
+        if ((y & 0x7F800000u) == 0x7F800000u) { y &= 0xFFFFu; odd = true; }
+    }
+    return odd;
+}
+
+// What all warps know of the unit at hand.
+struct Unit {
+    AttnSegment g;
+    int row_first, rows, upto, tile1, n_tiles, streams;
+    bool many;   // rows of the call that not all rows see
+};
+
+template <int D, bool TMA> __global__ void __launch_bounds__(AS_THREADS, 1)
+attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 {
     constexpr int TILE = as_tile_bytes<D>(), KS = D / 16, PIECES = D / 8;
     extern __shared__ __align__(16) unsigned char as_raw[];
@@ -98,10 +132,11 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
     const __nv_bfloat16 *k_cache = static_cast<const __nv_bfloat16 *>(p.k_cache), *v_cache = static_cast<const __nv_bfloat16 *>(p.v_cache);
 
     if (tid == 0) {
-        mbar_init(smem_u32(&sh.q_full), 32);
+        mbar_init(smem_u32(&sh.q_full), 256);
         for (int i = 0; i < AS_STAGES; ++i) {
-            mbar_init(smem_u32(&sh.k_full[i]), 32);
+            mbar_init(smem_u32(&sh.k_full[i]), TMA ? 1 : 32);
             mbar_init(smem_u32(&sh.v_full[i]), 32);
+            mbar_init(smem_u32(&sh.v_landed[i]), 1);
             mbar_init(smem_u32(&sh.k_empty[i]), 1);
             mbar_init(smem_u32(&sh.v_empty[i]), 1);
         }
@@ -137,59 +172,87 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
     // what has gone through the barriers before this unit: tiles, and tiles of the second stream; units
     uint32_t done = 0, done1 = 0, units = 0, units1 = 0;
     AttnWalk walk;
-    AttnSegment g;
     walk.begin(p, cta, AS_M, AS_TN);
-    while (walk.next(p, cta, AS_M, AS_TN, g)) {
-        __syncthreads();   // the unit before is through
-        if (*dead) break;
-        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, sh.anc, sh.anc_up)) {
-            if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
-            continue;
+    auto next_unit = [&](Unit &t) {   // by all threads together
+        for (;;) {
+            if (!walk.next(p, cta, AS_M, AS_TN, t.g)) return false;
+            __syncthreads();   // the unit before is through
+            if (*dead) return false;
+            if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, t.g.s, sh.anc, sh.anc_up)) {
+                if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
+                continue;
+            }
+            if (p.row_offsets && kind == AT_WORDS && !p.tree_ok[t.g.b]) continue;
+            t.row_first = t.g.m_tile * AS_M;
+            t.rows = min(AS_M, t.g.s.rows * p.group - t.row_first);
+            const int last_node = (t.row_first + t.rows - 1) / p.group;
+            t.upto = p.row_offsets ? t.g.s.len + last_node + 1 : t.g.s.len;
+            t.tile1 = min(t.g.tile1, max((t.upto + AS_TN - 1) / AS_TN, t.g.tile0));
+            t.n_tiles = t.tile1 - t.g.tile0;
+            t.many = p.row_offsets && t.g.s.rows > 1;
+            t.streams = t.rows > 128 ? 2 : 1;
+            if (tid == 0) sh.odd = 0;
+            __syncthreads();
+            return true;
         }
-        if (p.row_offsets && kind == AT_WORDS && !p.tree_ok[g.b]) continue;
-        const int row_first = g.m_tile * AS_M, rows = min(AS_M, g.s.rows * p.group - row_first);
-        const int last_node = (row_first + rows - 1) / p.group, upto = p.row_offsets ? g.s.len + last_node + 1 : g.s.len;
-        const int tile1 = min(g.tile1, max((upto + AS_TN - 1) / AS_TN, g.tile0)), n_tiles = tile1 - g.tile0;
-        const bool many = p.row_offsets && g.s.rows > 1;
-        const int streams = rows > 128 ? 2 : 1;
-        if (tid == 0) sh.odd = 0;
-        __syncthreads();
+    };
+    auto end_unit = [&](const Unit &t) {
+        done += t.n_tiles;
+        if (t.n_tiles > 0) ++units;
+        if (t.streams == 2) {
+            done1 += t.n_tiles;
+            if (t.n_tiles > 0) ++units1;
+        }
+    };
 
-        if (warp < 8) {   // ---- a row per thread
-            const int stream = warp >> 2;
-            if (stream < streams) {
-                const int r = tid, u = row_first + r, node = u / p.group;
-                const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + stream * 256, o_at = s_at + 128;
+    if (warp < 8) {   // ---- a row per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");   // (two groups of 216 and one of 72 are three of 168)
+        const int stream = warp >> 2;
+        const uint32_t s_at = tmem + ((uint32_t)((warp & 3) * 32) << 16) + stream * 256, o_at = s_at + 128;
+        Unit t;
+        while (next_unit(t)) {
+            const AttnSegment &g = t.g;
+            const int r = tid, u = t.row_first + r, node = u / p.group;
+            const bool mine = r < t.rows;
+            const size_t head = (size_t)(g.head * p.group + u % p.group);
+            if (t.n_tiles > 0) {
+                const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(p.q) + (mine ? (size_t)(g.s.row0 + node) * p.q_stride + head * D : 0);
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c) cp_async_16(q_s + stream * TILE + as_at(r & 127, c), src + c * 8, mine);
+                cp_async_wait_all();
+                fence_proxy_async();
+                mbar_arrive(smem_u32(&sh.q_full));
+            }
+            if (stream < t.streams) {
                 const uint32_t seen_before = stream ? done1 : done;
                 float m = -INFINITY, l = 0.f;   // m: of the raw scores, as the sums stand
                 bool ok = true;
-                for (int i = 0; i < n_tiles; ++i) {
+                for (int i = 0; i < t.n_tiles; ++i) {
                     const int tile = g.tile0 + i;
                     ok = wait(&sh.s_full[stream], (seen_before + i) & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    // bit j of word c: this row sees token tile * AS_TN + 32 c + j
-                    uint32_t see[4] = {~0u, ~0u, ~0u, ~0u};
-                    bool tail = (tile + 1) * AS_TN > g.s.len || stream * 128 + 128 > rows;
-                    if (tail) {
+                    uint32_t x[128];
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) see[c] = r < rows ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : 0;
-                        tail = __any_sync(0xffffffffu, (see[0] & see[1] & see[2] & see[3]) != ~0u);
-                    }
-                    float top = -INFINITY;
+                    for (int c = 0; c < 4; ++c) GDN_TMEM_LD32(s_at + c * 32, (x + c * 32));
+                    tmem_wait_ld();
+                    if ((tile + 1) * AS_TN > g.s.len || stream * 128 + 128 > t.rows) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32];
-                        GDN_TMEM_LD32(s_at + c * 32, x);
-                        tmem_wait_ld();
-                        if (tail) {
+                        for (int c = 0; c < 4; ++c) {   // bit j: this row sees token tile * AS_TN + 32 c + j
+                            const uint32_t see = mine ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : 0;
+                            if (__any_sync(0xffffffffu, see != ~0u)) {
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                if (!(see[c] >> j & 1)) x[j] = 0xFF800000u;
+                                for (int j = 0; j < 32; ++j)
+                                    if (!(see >> j & 1)) x[c * 32 + j] = 0xFF800000u;
+                            }
                         }
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) top = fmaxf(top, __uint_as_float(x[j]));
                     }
+                    float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                    for (int j = 0; j < 128; j += 8)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) t4[k] = fmaxf(fmaxf(t4[k], __uint_as_float(x[j + k])), __uint_as_float(x[j + 4 + k]));
+                    const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
                     const bool first = i == 0;
                     const bool raise = first || (top - m) * p.scale_log2 > AS_SLACK || (m == -INFINITY && top > -INFINITY);
                     float fade = 1.f;
@@ -200,32 +263,30 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
                         l *= fade;
                     }
                     if (!first && __any_sync(0xffffffffu, raise)) {
-#pragma unroll
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t x[32];
-                            GDN_TMEM_LD32(o_at + c * 32, x);
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t y[16];
+                            GDN_TMEM_LD16(o_at + c * 16, y);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) x[j] = __float_as_uint(__uint_as_float(x[j]) * fade);
-                            GDN_TMEM_ST32(o_at + c * 32, x);
+                            for (int j = 0; j < 16; ++j) y[j] = __float_as_uint(__uint_as_float(y[j]) * fade);
+                            GDN_TMEM_ST16(o_at + c * 16, y);
                         }
                     }
+                    // (a hidden score of -inf gives 2^-inf = 0; scale > 0 keeps it -inf)
                     const float ref = m == -INFINITY ? 0.f : m * p.scale_log2;
                     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        uint32_t x[32], w[16];
-                        GDN_TMEM_LD32(s_at + c * 32, x);
-                        tmem_wait_ld();
+                        uint32_t w[16];
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            float e = power_of_two(fmaf(__uint_as_float(x[j]), p.scale_log2, -ref));
-                            if (tail && !(see[c] >> j & 1)) e = 0.f;
-                            sum[j & 3] += e;
-                            x[j] = __float_as_uint(e);
+                        for (int j = 0; j < 16; ++j) {
+                            const float a = power_of_two(fmaf(__uint_as_float(x[c * 32 + 2 * j]), p.scale_log2, -ref));
+                            const float b = power_of_two(fmaf(__uint_as_float(x[c * 32 + 2 * j + 1]), p.scale_log2, -ref));
+                            sum[2 * (j & 1)] += a;
+                            sum[2 * (j & 1) + 1] += b;
+                            w[j] = pack_bf16(a, b);
                         }
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) w[j] = pack_bf16(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1]));
                         GDN_TMEM_ST16(s_at + c * 16, w);
                     }
                     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -233,28 +294,28 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
                     tc_fence_before();
                     mbar_arrive(smem_u32(&sh.p_full[stream]));
                 }
-                if (ok && n_tiles > 0) ok = wait(&sh.o_full[stream], (stream ? units1 : units) & 1);
+                if (ok && t.n_tiles > 0) ok = wait(&sh.o_full[stream], (stream ? units1 : units) & 1);
                 tc_fence_after();
                 if (ok) {
                     const bool odd = sh.odd != 0;
                     const float inv = l == 0.f ? 0.f : 1.f / l;
-                    __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + ((size_t)(g.s.row0 + node) * p.h_q + g.head * p.group + u % p.group) * D;
+                    __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + ((size_t)(g.s.row0 + node) * p.h_q + head) * D;
                     const size_t part = (size_t)(g.slot < 0 ? 0 : g.slot) * AS_M + r;
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t x[32];
-                        if (n_tiles > 0) {
+                        if (t.n_tiles > 0) {
                             GDN_TMEM_LD32(o_at + c * 32, x);
                             tmem_wait_ld();
                         } else {
 #pragma unroll
                             for (int j = 0; j < 32; ++j) x[j] = 0;
                         }
-                        if (odd && r < rows)
+                        if (odd && mine)
                             for (int j = 0; j <= node; ++j) {
-                                const int t = g.s.len + j;
-                                if (t < g.tile0 * AS_TN || t >= tile1 * AS_TN || !attn_sees(p, kind, sh.anc, g.s.row0, node, j)) continue;
-                                const long long at = attn_token_offset(p, g.b, t, upto);
+                                const int at_token = g.s.len + j;
+                                if (at_token < g.tile0 * AS_TN || at_token >= t.tile1 * AS_TN || !attn_sees(p, kind, sh.anc, g.s.row0, node, j)) continue;
+                                const long long at = attn_token_offset(p, g.b, at_token, t.upto);
                                 if (at < 0) continue;
                                 const __nv_bfloat16 *v = v_cache + at + g.head * p.head_stride + c * 32;
 #pragma unroll
@@ -263,7 +324,7 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
                                     if (!(fabsf(y) < INFINITY)) x[e] = __float_as_uint(__uint_as_float(x[e]) + y);
                                 }
                             }
-                        if (r >= rows) continue;
+                        if (!mine) continue;
                         if (g.slot < 0) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
@@ -279,155 +340,159 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
                                 *reinterpret_cast<uint4 *>(p.part_o + part * D + c * 32 + j * 4) = make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
                         }
                     }
-                    if (r < rows && g.slot >= 0)
+                    if (mine && g.slot >= 0)
                         *reinterpret_cast<float2 *>(p.part_ml + part * 2) = make_float2(m == -INFINITY ? m : m * p.scale_log2, l);
                 }
                 tc_fence_before();
             }
-        } else if (warp < 10) {   // ---- tiles, of keys or of values: 32 lanes, each with the places of four tokens
-            const bool keys = warp == 8;
-            constexpr int ROWS = 32 / PIECES;   // rows that one access of the warp covers
-            const int col = lane % PIECES;
-            const __nv_bfloat16 *from_head = (keys ? k_cache : v_cache) + g.head * p.head_stride + col * 8;
-            const uint32_t to = keys ? k_s : v_s;
-            unsigned long long *full = keys ? sh.k_full : sh.v_full, *empty = keys ? sh.k_empty : sh.v_empty;
-            int page[4];
-            auto ask = [&](int tile) {
+            end_unit(t);
+        }
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        Unit t;
+        while (next_unit(t)) {
+            const AttnSegment &g = t.g;
+            if (warp < 10) {   // ---- tiles, of keys or of values
+                const bool keys = warp == 8;
+                const uint32_t to = keys ? k_s : v_s;
+                unsigned long long *full = keys ? sh.k_full : sh.v_full, *empty = keys ? sh.k_empty : sh.v_empty;
+                constexpr int ASKS = TMA ? 1 : 4;   // places that a lane looks up: of its box, or of four tokens
+                const int box = TMA ? maps.box : 1;
+                int page[ASKS];
+                auto token_of = [&](int tile, int k) { return tile * AS_TN + (TMA ? lane * box : k * 32 + lane); };
+                auto ask = [&](int tile) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int t = tile * AS_TN + k * 32 + lane;
-                    page[k] = tile < tile1 && t < upto
-                                  ? p.page_table[(size_t)g.b * p.max_pages + (p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size)] : -1;
-                }
-            };
-            ask(g.tile0);
-            for (int i = 0; i < n_tiles; ++i) {
-                const uint32_t n = done + i;
-                const int stage = n % AS_STAGES, tile = g.tile0 + i;
-                long long place[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int t = tile * AS_TN + k * 32 + lane;
-                    place[k] = -1;
-                    if (t < upto) {
-                        if (page[k] < 0 || page[k] >= p.n_pages) report_status(p.status_dev, GDN_ERR_PAGE);
-                        else place[k] = page[k] * p.page_stride + (p.page_shift >= 0 ? t & (p.page_size - 1) : t % p.page_size) * p.token_stride;
+                    for (int k = 0; k < ASKS; ++k) {
+                        const int token = token_of(tile, k);
+                        page[k] = tile < t.tile1 && token < t.upto && (!TMA || lane * box < AS_TN)
+                                      ? p.page_table[(size_t)g.b * p.max_pages + (p.page_shift >= 0 ? token >> p.page_shift : token / p.page_size)] : -1;
                     }
-                }
-                ask(tile + 1);
-                if (n >= AS_STAGES && !wait(&empty[stage], (n / AS_STAGES - 1) & 1)) break;
+                };
+                ask(g.tile0);
+                for (int i = 0; i < t.n_tiles; ++i) {
+                    const uint32_t n = done + i;
+                    const int stage = n % AS_STAGES, tile = g.tile0 + i;
+                    bool good[ASKS];
+                    int in_page[ASKS], at_page[ASKS];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
+                    for (int k = 0; k < ASKS; ++k) {
+                        const int token = token_of(tile, k);
+                        const bool wanted = token < t.upto && (!TMA || lane * box < AS_TN);
+                        good[k] = wanted && page[k] >= 0 && page[k] < p.n_pages;
+                        if (wanted && !good[k]) report_status(p.status_dev, GDN_ERR_PAGE);
+                        at_page[k] = page[k];
+                        in_page[k] = p.page_shift >= 0 ? token & (p.page_size - 1) : token % p.page_size;
+                    }
+                    ask(tile + 1);
+                    if (n >= AS_STAGES && !wait(&empty[stage], (n / AS_STAGES - 1) & 1)) break;
+                    if constexpr (TMA) {
+                        const uint32_t bar = smem_u32(keys ? &sh.k_full[stage] : &sh.v_landed[stage]);
+                        if (lane == 0) mbar_expect_tx(bar, TILE);
+                        __syncwarp();
+                        if (lane * box < AS_TN)   // (a page behind the last one reads as zeros)
+#pragma unroll
+                            for (int c = 0; c < D / 64; ++c)
+                                tma_load_4d(to + stage * TILE + c * (AS_TN * 128) + lane * box * 128, keys ? &maps.k : &maps.v, c * 64, in_page[0], g.head,
+                                            good[0] ? at_page[0] : p.n_pages, bar);
+                        if (!keys && !wait(&sh.v_landed[stage], (n / AS_STAGES) & 1)) break;
+                    } else {
+                        constexpr int ROWS = 32 / PIECES;   // rows that one access of the warp covers
+                        const int col = lane % PIECES;
+                        const __nv_bfloat16 *from_head = (keys ? k_cache : v_cache) + g.head * p.head_stride + col * 8;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const long long place = good[k] ? at_page[k] * p.page_stride + in_page[k] * p.token_stride : -1;
 #pragma unroll 8
-                    for (int h = 0; h < 32 / ROWS; ++h) {
-                        const int in = h * ROWS + lane / PIECES;
-                        const long long at = __shfl_sync(0xffffffffu, place[k], in);
-                        cp_async_16(to + stage * TILE + as_at(k * 32 + in, col), from_head + (at < 0 ? 0 : at), at >= 0);
-                    }
-                cp_async_wait_all();
-                if (!keys && many && (tile + 1) * AS_TN > g.s.len)   // (an infinite value times a weight of 0 is no number: see the end of a unit)
-                    for (int k = 0; k < AS_TN / ROWS; ++k) {
-                        const int row = k * ROWS + lane / PIECES, t = tile * AS_TN + row;
-                        if (t < g.s.len || t >= upto) continue;
-                        uint4 *at = reinterpret_cast<uint4 *>(data + (v_s - q_s) + stage * TILE + as_at(row, col));   // (as this lane has copied it)
-                        uint4 x = *at;
-                        bool odd = false;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            uint32_t &y = (&x.x)[e];
-                            if ((y & 0x7F80u) == 0x7F80u) { y &= 0xFFFF0000u; odd = true; }
-                            if ((y & 0x7F800000u) == 0x7F800000u) { y &= 0xFFFFu; odd = true; }
+                            for (int h = 0; h < 32 / ROWS; ++h) {
+                                const int in = h * ROWS + lane / PIECES;
+                                const long long at = __shfl_sync(0xffffffffu, place, in);
+                                cp_async_16(to + stage * TILE + as_at(k * 32 + in, col), from_head + (at < 0 ? 0 : at), at >= 0);
+                            }
                         }
-                        if (odd) {
-                            *at = x;
-                            sh.odd = 1;
-                        }
+                        cp_async_wait_all();
+                        __syncwarp();
                     }
-                fence_proxy_async();
-                mbar_arrive(smem_u32(&full[stage]));
-            }
-        } else if (warp == 11) {   // ---- queries of the streams
-            if (n_tiles > 0) {
-#pragma unroll 8
-                for (int i = lane; i < streams * 128 * PIECES; i += 32) {
-                    const int r = i / PIECES, c = i % PIECES, u = row_first + r;
-                    const __nv_bfloat16 *src = static_cast<const __nv_bfloat16 *>(p.q);
-                    if (r < rows) src += (size_t)(g.s.row0 + u / p.group) * p.q_stride + (size_t)(g.head * p.group + u % p.group) * D + c * 8;
-                    cp_async_16(q_s + (r >> 7) * TILE + as_at(r & 127, c), src, r < rows);
+                    // values of places that hold no token: zeros (their weights are 0, and 0 times what lies there may be no number); of rows of
+                    // the call that not every row sees: what is infinite or no number is taken out, and added at the end of the unit
+                    if (!keys && (tile + 1) * AS_TN > (t.many ? g.s.len : t.upto)) {
+                        for (int k = lane; k < AS_TN * PIECES; k += 32) {
+                            const int row = k / PIECES, token = tile * AS_TN + row;
+                            if (token < g.s.len && token < t.upto) continue;
+                            uint4 *at = reinterpret_cast<uint4 *>(data + (v_s - q_s) + stage * TILE + as_at(row, k % PIECES));
+                            uint4 y = *at;
+                            if (token >= t.upto) *at = make_uint4(0, 0, 0, 0);
+                            else if (zero_odd(y)) {
+                                *at = y;
+                                sh.odd = 1;
+                            }
+                        }
+                        __syncwarp();
+                    }
+                    if (!TMA || !keys) {
+                        fence_proxy_async();
+                        mbar_arrive(smem_u32(&full[stage]));
+                    }
                 }
-                cp_async_wait_all();
-                fence_proxy_async();
-                mbar_arrive(smem_u32(&sh.q_full));
-            }
-        } else if (n_tiles > 0) {   // ---- products
-            constexpr uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, D) | (1u << 16);
-            bool ok = wait(&sh.q_full, units & 1);
-            auto scores = [&](int s, int i) {
-                const uint32_t k_at = k_s + ((done + i) % AS_STAGES) * TILE, q_at = q_s + s * TILE;
-                if (elect_one()) {
-#pragma unroll
-                    for (int k = 0; k < KS; ++k)
-                        umma_bf16(tmem + s * 256, smem_desc_sw128(q_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32),
-                                  smem_desc_sw128(k_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32), id_s, k != 0);
-                    umma_commit(smem_u32(&sh.s_full[s]));
-                }
-                __syncwarp();
-            };
-            ok = ok && wait(&sh.k_full[done % AS_STAGES], (done / AS_STAGES) & 1);
-            tc_fence_after();
-            if (ok) {
-                for (int s = 0; s < streams; ++s) scores(s, 0);
-                if (elect_one()) umma_commit(smem_u32(&sh.k_empty[done % AS_STAGES]));
-                __syncwarp();
-            }
-            for (int i = 0; i < n_tiles && ok; ++i) {
-                const uint32_t n = done + i, next = n + 1;
-                const int stage = n % AS_STAGES;
-                ok = wait(&sh.v_full[stage], (n / AS_STAGES) & 1);
-                for (int s = 0; s < streams && ok; ++s) {
-                    ok = wait(&sh.p_full[s], ((s ? done1 : done) + i) & 1);
-                    if (!ok) break;
-                    tc_fence_after();
+            } else if (warp == 10 && t.n_tiles > 0) {   // ---- products
+                constexpr uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, D) | (1u << 16);
+                bool ok = wait(&sh.q_full, units & 1);
+                auto scores = [&](int s, int i) {
+                    const uint32_t k_at = k_s + ((done + i) % AS_STAGES) * TILE, q_at = q_s + s * TILE;
                     if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < AS_TN / 16; ++k)
-                            umma_bf16_ts_into(tmem + s * 256 + 128, tmem + s * 256 + k * 8, desc_rows_along_k(v_s + stage * TILE + k * 2048), id_o,
-                                              i > 0 || k > 0);
-                        if (i + 1 == n_tiles) umma_commit(smem_u32(&sh.o_full[s]));
+                        for (int k = 0; k < KS; ++k)
+                            umma_bf16(tmem + s * 256, smem_desc_sw128(q_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32),
+                                      smem_desc_sw128(k_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32), id_s, k != 0);
+                        umma_commit(smem_u32(&sh.s_full[s]));
                     }
                     __syncwarp();
-                    if (i + 1 < n_tiles) {
-                        if (s == 0) {
-                            ok = wait(&sh.k_full[next % AS_STAGES], (next / AS_STAGES) & 1);
-                            tc_fence_after();
+                };
+                ok = ok && wait(&sh.k_full[done % AS_STAGES], (done / AS_STAGES) & 1);
+                tc_fence_after();
+                if (ok) {
+                    for (int s = 0; s < t.streams; ++s) scores(s, 0);
+                    if (elect_one()) umma_commit(smem_u32(&sh.k_empty[done % AS_STAGES]));
+                    __syncwarp();
+                }
+                for (int i = 0; i < t.n_tiles && ok; ++i) {
+                    const uint32_t n = done + i, next = n + 1;
+                    const int stage = n % AS_STAGES;
+                    ok = wait(&sh.v_full[stage], (n / AS_STAGES) & 1);
+                    for (int s = 0; s < t.streams && ok; ++s) {
+                        ok = wait(&sh.p_full[s], ((s ? done1 : done) + i) & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < AS_TN / 16; ++k)
+                                umma_bf16_ts_into(tmem + s * 256 + 128, tmem + s * 256 + k * 8, desc_rows_along_k(v_s + stage * TILE + k * 2048), id_o,
+                                                  i > 0 || k > 0);
+                            if (i + 1 == t.n_tiles) umma_commit(smem_u32(&sh.o_full[s]));
                         }
-                        if (ok) scores(s, i + 1);
+                        __syncwarp();
+                        if (i + 1 < t.n_tiles) {
+                            if (s == 0) {
+                                ok = wait(&sh.k_full[next % AS_STAGES], (next / AS_STAGES) & 1);
+                                tc_fence_after();
+                            }
+                            if (ok) scores(s, i + 1);
+                        }
                     }
+                    if (ok && elect_one()) {
+                        umma_commit(smem_u32(&sh.v_empty[stage]));
+                        if (i + 1 < t.n_tiles) umma_commit(smem_u32(&sh.k_empty[next % AS_STAGES]));
+                    }
+                    __syncwarp();
                 }
-                if (ok && elect_one()) {
-                    umma_commit(smem_u32(&sh.v_empty[stage]));
-                    if (i + 1 < n_tiles) umma_commit(smem_u32(&sh.k_empty[next % AS_STAGES]));
-                }
-                __syncwarp();
             }
-        }
-        done += n_tiles;
-        if (n_tiles > 0) ++units;
-        if (streams == 2) {
-            done1 += n_tiles;
-            if (n_tiles > 0) ++units1;
+            end_unit(t);
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (*dead) {   // products may still be on their way: behind them all comes this one's arrival
-        if (warp == 10) {
-            tc_fence_after();
-            if (elect_one()) umma_commit(smem_u32(&sh.q_full));
-            __syncwarp();
-            const long long t0 = clock64();
-            while (clock64() - t0 < 2000000) {}   // a millisecond, far longer than what can be in the queue takes
-        }
+    if (*dead) {   // products and copies may still be on their way: a millisecond, far longer than what can be in their queues takes
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000) {}
         __syncthreads();
     }
     if (warp == 10) {
@@ -436,19 +501,36 @@ template <int D> __global__ void __launch_bounds__(AS_THREADS, 1) attn_sm100_ker
     }
 }
 
+bool cache_map(CUtensorMap *tm, const void *cache, const AttnParams &p, int box)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)p.d, (cuuint64_t)p.page_size, (cuuint64_t)p.h_kv, (cuuint64_t)p.n_pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)p.token_stride * 2, (cuuint64_t)p.head_stride * 2, (cuuint64_t)p.page_stride * 2};
+    const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1}, steps[4] = {1, 1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(cache), dims, strides, boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 AttnTiling attn_sm100_tiling() { return {AS_M, AS_TN, 1}; }
 
 cudaError_t launch_attn_sm100(const AttnParams &p, int grid, cudaStream_t stream)
 {
-    static PerContext seen[2];
-    const auto kernel = p.d == 128 ? attn_sm100_kernel<128> : attn_sm100_kernel<64>;
+    static PerContext seen[4];
+    using Kernel = void (*)(const AttnParams, const CacheMaps);
+    static const Kernel kernels[4] = {attn_sm100_kernel<64, false>, attn_sm100_kernel<64, true>, attn_sm100_kernel<128, false>, attn_sm100_kernel<128, true>};
+    CacheMaps maps{};
+    maps.box = p.page_size < AS_TN ? p.page_size : AS_TN;
+    // (swizzled boxes begin on 1024 bytes, so that one has eight rows or more; strides that a tensor map cannot have are the other kernel's)
+    const bool tma = p.page_shift >= 3 && cache_map(&maps.k, p.k_cache, p, maps.box) && cache_map(&maps.v, p.v_cache, p, maps.box);
+    const int which = (p.d == 128 ? 2 : 0) + (tma ? 1 : 0);
     const size_t smem = p.d == 128 ? as_smem<128>() : as_smem<64>();
     int sms = 0;
-    const cudaError_t e = device_sms(seen[p.d == 128], reinterpret_cast<const void *>(kernel), smem, &sms);
+    const cudaError_t e = device_sms(seen[which], reinterpret_cast<const void *>(kernels[which]), smem, &sms);
     if (e != cudaSuccess) return e;
-    return launch_behind(kernel, dim3((unsigned)grid), AS_THREADS, smem, stream, p);
+    return launch_behind(kernels[which], dim3((unsigned)grid), AS_THREADS, smem, stream, p, maps);
 }
 
 }  // namespace gdn
