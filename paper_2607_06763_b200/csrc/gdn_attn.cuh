@@ -32,7 +32,7 @@ struct AttnParams {
     uint32_t *mask;                                  // [total_rows][mask_words]
     int mask_words;
     int32_t *tree_ok;                                // [n_seq]
-    float *part_o, *part_ml;                         // [2 * CTAs][M][d], [2 * CTAs][M][2]
+    float *part_o, *part_ml;                         // [2 * CTAs][M * d], [2 * CTAs][M][2]: sums; maximum, denominator
     int n_ctas;
 };
 
@@ -272,7 +272,8 @@ cudaError_t launch_attn_rows(const AttnParams &p, int M, int grid, cudaStream_t 
 AttnTiling attn_sm100_tiling();
 cudaError_t launch_attn_sm100(const AttnParams &p, int grid, cudaStream_t stream);
 cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream);
-cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream);
+// columns_first: parts lie [d / 4][M][4], not [M][d].
+cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, bool columns_first, cudaStream_t stream);
 
 cudaError_t launch_kv_append(const AttnParams &a, bool bf16, const void *k, const void *v, long long k_stride, long long v_stride,
                              const float *rope, int rope_dim, bool interleaved, void *q_out, void *k_out, void *v_out,

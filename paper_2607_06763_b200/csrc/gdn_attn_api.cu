@@ -126,7 +126,7 @@ int attention(const gdn_attn_shape_t *shape, const void *q, const void *k_cache,
                           : c.kernel == Choice::ROWS  ? launch_attn_rows(p, c.tiling.M, c.grid, stream)
                                                       : launch_attn_sm100(p, c.grid, stream);
     if (e != cudaSuccess) return GDN_ERR_CUDA;
-    if (c.split && launch_attn_join(p, bf16, c.tiling.M, c.tiling.TN, stream) != cudaSuccess) return GDN_ERR_CUDA;
+    if (c.split && launch_attn_join(p, bf16, c.tiling.M, c.tiling.TN, c.kernel == Choice::SM100, stream) != cudaSuccess) return GDN_ERR_CUDA;
     return GDN_OK;
 }
 

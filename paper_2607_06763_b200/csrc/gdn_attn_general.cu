@@ -211,30 +211,19 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mask_kernel(const AttnParams 
 }
 
 // The parts of a split unit, in the order of their tiles, to its rows: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
-// One warp per row, the CTAs of a unit eight rows each; a unit that one run held is left alone.
-constexpr int AJ_THREADS = 256;
-template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_kernel(const AttnParams p, int M, int TN)
+// A thread has four components of a row; the threads of a CTA read neighbouring pieces of each part, which lie [M][d / 4] or, where a
+// thread of the kernel in front has a row (columns_first), [d / 4][M].  A unit that one run held is left alone.
+constexpr int AJ_THREADS = 128;
+template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_kernel(const AttnParams p, int M, int TN, int columns_first)
 {
     wait_for_previous_kernel();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31;
     const int units = p.h_kv * p.m_tiles, b = (int)blockIdx.x / units, head = (int)blockIdx.x % units / p.m_tiles, m_tile = (int)blockIdx.x % p.m_tiles;
-    AttnSeq s;
-    if (!attn_seq(p, b, s, false)) return;
-    const int row_first = m_tile * M, row = (int)blockIdx.y * 8 + warp, rows = min(M, s.rows * p.group - row_first);
-    if ((int)blockIdx.y * 8 >= rows) return;
-    if (p.row_offsets && p.parent) {
-        if (p.max_rows > AT_SMALL_ROWS) {
-            if (!p.tree_ok[b]) return;
-        } else {
-            bool bad = false;
-            if ((int)threadIdx.x < s.rows) {
-                const int parent = p.parent[s.row0 + threadIdx.x];
-                bad = parent < -1 || parent >= (int)threadIdx.x;
-            }
-            if (__syncthreads_or(bad)) return;
-        }
-    }
+    const int piece = (int)blockIdx.y * AJ_THREADS + (int)threadIdx.x, pieces = p.d / 4;
+    const int row = columns_first ? piece % M : piece / pieces, column = columns_first ? piece / M : piece % pieces;
     // the first tile of this unit among those of all units, as AttnWalk counts them
+    AttnSeq s;
+    const bool fits = attn_seq(p, b, s, false);
     const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
     long long mine = 0, before = 0;
     for (int i = b0; i < b1; ++i) {
@@ -249,39 +238,49 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
         total += __shfl_xor_sync(0xffffffffu, total, off);
         before += __shfl_xor_sync(0xffffffffu, before, off);
     }
+    if (!fits) return;
+    const int row_first = m_tile * M, rows = min(M, s.rows * p.group - row_first);
+    if (rows <= 0) return;
+    if (p.row_offsets && p.parent) {
+        if (p.max_rows > AT_SMALL_ROWS) {
+            if (!p.tree_ok[b]) return;
+        } else {
+            bool bad = false;
+            if ((int)threadIdx.x < s.rows) {
+                const int parent = p.parent[s.row0 + threadIdx.x];
+                bad = parent < -1 || parent >= (int)threadIdx.x;
+            }
+            if (__syncthreads_or(bad)) return;
+        }
+    }
     const int tiles = attn_tiles(s, TN), m_tiles = (s.rows * p.group + M - 1) / M;
     const long long first = before + (long long)(head * m_tiles + m_tile) * tiles, last = first + tiles - 1;
     const long long runs = total < p.n_ctas ? total : p.n_ctas;
     const int c0 = (int)(((first + 1) * runs - 1) / total), c1 = (int)(((last + 1) * runs - 1) / total);
-    if (c0 == c1 || row >= rows) return;
+    if (c0 == c1 || row >= rows || column >= pieces) return;
 
+    auto slot = [&](int c) { return (size_t)(c == c0 ? 2 * c + 1 : 2 * c); };
     float m = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) m = fmaxf(m, p.part_ml[((size_t)(c == c0 ? 2 * c + 1 : 2 * c) * M + row) * 2]);
-#pragma unroll
-    for (int off = 16; off; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+#pragma unroll 8
+    for (int c = c0; c <= c1; ++c) m = fmaxf(m, p.part_ml[(slot(c) * M + row) * 2]);
     const float ref = m == -INFINITY ? 0.f : m;
     float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int c = c0; c <= c1; ++c) {
-        const size_t at = (size_t)(c == c0 ? 2 * c + 1 : 2 * c) * M + row;
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + at * 2);
-        const float f = exp2f(ml.x - ref);
+        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + (slot(c) * M + row) * 2);
+        const float4 v = *reinterpret_cast<const float4 *>(p.part_o + (slot(c) * M * pieces + piece) * 4);
+        const float f = power_of_two(ml.x - ref);
         l = fmaf(f, ml.y, l);
-        if (lane * 4 < p.d && ml.x != -INFINITY) {
-            const float4 v = *reinterpret_cast<const float4 *>(p.part_o + at * p.d + lane * 4);
-            acc[0] = fmaf(f, v.x, acc[0]);
-            acc[1] = fmaf(f, v.y, acc[1]);
-            acc[2] = fmaf(f, v.z, acc[2]);
-            acc[3] = fmaf(f, v.w, acc[3]);
-        }
+        acc[0] = fmaf(f, v.x, acc[0]);
+        acc[1] = fmaf(f, v.y, acc[1]);
+        acc[2] = fmaf(f, v.z, acc[2]);
+        acc[3] = fmaf(f, v.w, acc[3]);
     }
-    if (lane * 4 < p.d) {
-        const int u = row_first + row;
-        T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + lane * 4;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) store_from_float(o + c, acc[c] * inv);
-    }
+    const int u = row_first + row;
+    T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + column * 4;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    else *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
 }
 
 }  // namespace
@@ -292,11 +291,11 @@ cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream)
                          (size_t)p.max_rows * sizeof(int), stream, p);
 }
 
-cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, cudaStream_t stream)
+cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, bool columns_first, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)(p.n_seq * p.h_kv * p.m_tiles), (unsigned)((min(M, p.max_rows * p.group) + 7) / 8));
-    return bf16 ? launch_behind(attn_join_kernel<__nv_bfloat16>, grid, AJ_THREADS, 0, stream, p, M, TN)
-                : launch_behind(attn_join_kernel<float>, grid, AJ_THREADS, 0, stream, p, M, TN);
+    const int rows = columns_first ? M : min(M, p.max_rows * p.group);
+    const dim3 grid((unsigned)(p.n_seq * p.h_kv * p.m_tiles), (unsigned)((rows * (p.d / 4) + AJ_THREADS - 1) / AJ_THREADS));
+    return launch_behind(bf16 ? attn_join_kernel<__nv_bfloat16> : attn_join_kernel<float>, grid, AJ_THREADS, 0, stream, p, M, TN, columns_first ? 1 : 0);
 }
 
 AttnTiling attn_general_tiling() { return {AG_M, AG_TN, 3}; }

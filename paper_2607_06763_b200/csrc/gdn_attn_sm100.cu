@@ -10,8 +10,8 @@
 // weights up to 256 are as exact in bf16, and O is multiplied only where a row's maximum has risen by more.
 //
 // Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, warp 10 the products.
-// Two stages of keys and of values, each with its own barriers.  Pages of 8 tokens or more, in powers of two, come by tensor copies, a
-// page or a part of one each, straight into the swizzled layout of the products' operands; others by cp.async, row by row: one warp needs
+// Two stages of keys and of values, each with its own barriers.  Pages whose size is a multiple of 8 come by tensor copies, a page
+// or a part of one each, straight into the swizzled layout of the products' operands; others by cp.async, row by row: one warp needs
 // 3300 clocks to issue a tile that way, the products of two streams 2048.
 // A row's 128 scores stay in its thread's registers (the warps of the rows take over what the others leave).
 // Every wait is bounded; one that expires raises a flag that ends the others.
@@ -31,7 +31,7 @@ template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t
 struct SplitShared {
     unsigned long long anc[AT_SMALL_ROWS];
     int anc_up[AT_SMALL_ROWS];
-    unsigned long long q_full, k_full[AS_STAGES], v_full[AS_STAGES], v_landed[AS_STAGES], k_empty[AS_STAGES], v_empty[AS_STAGES], s_full[2], p_full[2], o_full[2];
+    unsigned long long q_full, k_full[AS_STAGES], v_full[AS_STAGES], v_landed[AS_STAGES], k_empty[AS_STAGES], v_empty[AS_STAGES], s_full[2], p_full[2][2], o_full[2];   // p_full: [half of the tile][stream]
     uint32_t tmem;
     int odd, dead;
 };
@@ -94,6 +94,9 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm,
                  ::"r"(dst), "l"(tm), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
 }
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 struct CacheMaps {
     CUtensorMap k, v;   // [page][head][token][component], boxes of 64 components of `box` tokens
     int box;
@@ -110,6 +113,39 @@ __device__ __forceinline__ bool zero_odd(uint4 &u)
         if ((y & 0x7F800000u) == 0x7F800000u) { y &= 0xFFFFu; odd = true; }
     }
     return odd;
+}
+
+// Two fp32 operations at once.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// 2^x of two numbers of at most 2^7 without the special function unit, which forms 16 per clock and SM where a tile pair's products
+// leave time for 32768 / 2048: x = n + r, |r| <= 1/2, 2^r by the polynomial of degree 3 with p(0) = 1 that is off by the least
+// relative error there, 1.0e-4 (fitted to 2^r; a twentieth of the step of the bf16 weights), and n into the exponent.  Below
+// 2^-126 the result stays there: not for scores that are hidden.
+__device__ __forceinline__ float2 power_of_two_by_products(float2 x)
+{
+    x.x = fmaxf(x.x, -126.f);
+    x.y = fmaxf(x.y, -126.f);
+    const float2 big = make_float2(12582912.f, 12582912.f);   // 1.5 * 2^23: rounds to whole numbers, which stand in the low bits
+    const float2 n = add2(x, big);
+    const float2 r = add2(x, fma2(n, make_float2(-1.f, -1.f), big));
+    float2 y = fma2(r, make_float2(0.05500893294811249f, 0.05500893294811249f), make_float2(0.2422109693288803f, 0.2422109693288803f));
+    y = fma2(r, y, make_float2(0.6932829022407532f, 0.6932829022407532f));
+    y = fma2(r, y, make_float2(1.f, 1.f));
+    return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
 }
 
 // What all warps know of the unit at hand.
@@ -142,7 +178,8 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
-            mbar_init(smem_u32(&sh.p_full[i]), 128);
+            mbar_init(smem_u32(&sh.p_full[0][i]), 128);
+            mbar_init(smem_u32(&sh.p_full[1][i]), 128);
             mbar_init(smem_u32(&sh.o_full[i]), 1);
         }
         sh.dead = 0;
@@ -155,7 +192,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
     const uint32_t tmem = sh.tmem;   // stream s: S (and P over it) at columns s * 256, O at s * 256 + 128
     volatile int *dead = &sh.dead;
 
-    auto wait = [&](unsigned long long *bar, uint32_t parity) {   // by a whole warp; false: expired here or elsewhere
+    auto wait_alone = [&](unsigned long long *bar, uint32_t parity) {   // false: expired here or elsewhere
         const uint32_t at = smem_u32(bar);
         bool there = mbar_try_wait(at, parity);
         if (!there) {
@@ -166,8 +203,9 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                     report_status(p.status_dev, GDN_ERR_TIMEOUT);
                 }
         }
-        return __all_sync(0xffffffffu, there) != 0;
+        return there;
     };
+    auto wait = [&](unsigned long long *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_alone(bar, parity)) != 0; };   // by a whole warp
 
     // what has gone through the barriers before this unit: tiles, and tiles of the second stream; units
     uint32_t done = 0, done1 = 0, units = 0, units1 = 0;
@@ -236,15 +274,18 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) GDN_TMEM_LD32(s_at + c * 32, (x + c * 32));
                     tmem_wait_ld();
-                    if ((tile + 1) * AS_TN > g.s.len || stream * 128 + 128 > t.rows) {
+                    bool hidden = (tile + 1) * AS_TN > g.s.len || stream * 128 + 128 > t.rows;   // from some row of this warp, some token
+                    if (hidden) {
+                        uint32_t see[4], all = ~0u;   // bit j: this row sees token tile * AS_TN + 32 c + j
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {   // bit j: this row sees token tile * AS_TN + 32 c + j
-                            const uint32_t see = mine ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : 0;
-                            if (__any_sync(0xffffffffu, see != ~0u)) {
+                        for (int c = 0; c < 4; ++c) all &= see[c] = mine ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : 0;
+                        hidden = __any_sync(0xffffffffu, all != ~0u);
+                        if (hidden) {
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
 #pragma unroll
                                 for (int j = 0; j < 32; ++j)
-                                    if (!(see >> j & 1)) x[c * 32 + j] = 0xFF800000u;
-                            }
+                                    if (!(see[c] >> j & 1)) x[c * 32 + j] = 0xFF800000u;
                         }
                     }
                     float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -275,24 +316,31 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                     }
                     // (a hidden score of -inf gives 2^-inf = 0; scale > 0 keeps it -inf)
                     const float ref = m == -INFINITY ? 0.f : m * p.scale_log2;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    const float2 scale2 = make_float2(p.scale_log2, p.scale_log2), ref2 = make_float2(-ref, -ref);
+                    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t w[16];
+                        auto weights = [&](auto by_products) {   // three of eight pairs go without the special function unit
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float a = power_of_two(fmaf(__uint_as_float(x[c * 32 + 2 * j]), p.scale_log2, -ref));
-                            const float b = power_of_two(fmaf(__uint_as_float(x[c * 32 + 2 * j + 1]), p.scale_log2, -ref));
-                            sum[2 * (j & 1)] += a;
-                            sum[2 * (j & 1) + 1] += b;
-                            w[j] = pack_bf16(a, b);
-                        }
+                            for (int j = 0; j < 16; ++j) {
+                                float2 e = fma2(make_float2(__uint_as_float(x[c * 32 + 2 * j]), __uint_as_float(x[c * 32 + 2 * j + 1])), scale2, ref2);
+                                if (decltype(by_products)::value && (j % 8 == 1 || j % 8 == 4 || j % 8 == 7)) e = power_of_two_by_products(e);
+                                else e = make_float2(power_of_two(e.x), power_of_two(e.y));
+                                sum[j & 1] = add2(sum[j & 1], e);
+                                w[j] = pack_bf16(e.x, e.y);
+                            }
+                        };
+                        if (hidden) weights(No{});
+                        else weights(Yes{});
                         GDN_TMEM_ST16(s_at + c * 16, w);
+                        if (c == 1 || c == 3) {   // half of the tile's weights: their part of the second product may begin
+                            tmem_wait_st();
+                            tc_fence_before();
+                            mbar_arrive(smem_u32(&sh.p_full[c >> 1][stream]));
+                        }
                     }
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_wait_st();
-                    tc_fence_before();
-                    mbar_arrive(smem_u32(&sh.p_full[stream]));
+                    l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
                 }
                 if (ok && t.n_tiles > 0) ok = wait(&sh.o_full[stream], (stream ? units1 : units) & 1);
                 tc_fence_after();
@@ -300,7 +348,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                     const bool odd = sh.odd != 0;
                     const float inv = l == 0.f ? 0.f : 1.f / l;
                     __nv_bfloat16 *o = static_cast<__nv_bfloat16 *>(p.o) + ((size_t)(g.s.row0 + node) * p.h_q + head) * D;
-                    const size_t part = (size_t)(g.slot < 0 ? 0 : g.slot) * AS_M + r;
+                    const size_t part = (size_t)(g.slot < 0 ? 0 : g.slot) * AS_M;
 #pragma unroll 1
                     for (int c = 0; c < D / 32; ++c) {
                         uint32_t x[32];
@@ -336,12 +384,13 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                             }
                         } else {
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                *reinterpret_cast<uint4 *>(p.part_o + part * D + c * 32 + j * 4) = make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                            for (int j = 0; j < 8; ++j)   // [slot][D / 4][M][4]: a warp's rows lie side by side
+                                *reinterpret_cast<uint4 *>(p.part_o + part * D + ((size_t)(c * 8 + j) * AS_M + r) * 4) =
+                                    make_uint4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
                         }
                     }
                     if (mine && g.slot >= 0)
-                        *reinterpret_cast<float2 *>(p.part_ml + part * 2) = make_float2(m == -INFINITY ? m : m * p.scale_log2, l);
+                        *reinterpret_cast<float2 *>(p.part_ml + (part + r) * 2) = make_float2(m == -INFINITY ? m : m * p.scale_log2, l);
                 }
                 tc_fence_before();
             }
@@ -433,57 +482,59 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         mbar_arrive(smem_u32(&full[stage]));
                     }
                 }
-            } else if (warp == 10 && t.n_tiles > 0) {   // ---- products
-                constexpr uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, D) | (1u << 16);
-                bool ok = wait(&sh.q_full, units & 1);
-                auto scores = [&](int s, int i) {
-                    const uint32_t k_at = k_s + ((done + i) % AS_STAGES) * TILE, q_at = q_s + s * TILE;
-                    if (elect_one()) {
+            } else if (warp == 10 && t.n_tiles > 0) {   // ---- products, by one thread: what it does between two of them the tensor cores may wait for
+                if (elect_one()) {
+                    constexpr uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, D) | (1u << 16);
+                    auto scores = [&](int s, uint32_t n) {
+                        const uint64_t q_d = smem_desc_sw128(q_s + s * TILE), k_d = smem_desc_sw128(k_s + (n % AS_STAGES) * TILE);
 #pragma unroll
-                        for (int k = 0; k < KS; ++k)
-                            umma_bf16(tmem + s * 256, smem_desc_sw128(q_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32),
-                                      smem_desc_sw128(k_at + (k >> 2) * (AS_TN * 128) + (k & 3) * 32), id_s, k != 0);
+                        for (int k = 0; k < KS; ++k) {
+                            const uint64_t on = ((k >> 2) * (AS_TN * 128) + (k & 3) * 32) >> 4;
+                            umma_bf16(tmem + s * 256, q_d + on, k_d + on, id_s, k != 0);
+                        }
                         umma_commit(smem_u32(&sh.s_full[s]));
+                    };
+                    bool ok = wait_alone(&sh.q_full, units & 1) && wait_alone(&sh.k_full[done % AS_STAGES], (done / AS_STAGES) & 1);
+                    tc_fence_after();
+                    if (ok) {
+                        for (int s = 0; s < t.streams; ++s) scores(s, done);
+                        umma_commit(smem_u32(&sh.k_empty[done % AS_STAGES]));
                     }
-                    __syncwarp();
-                };
-                ok = ok && wait(&sh.k_full[done % AS_STAGES], (done / AS_STAGES) & 1);
-                tc_fence_after();
-                if (ok) {
-                    for (int s = 0; s < t.streams; ++s) scores(s, 0);
-                    if (elect_one()) umma_commit(smem_u32(&sh.k_empty[done % AS_STAGES]));
-                    __syncwarp();
-                }
-                for (int i = 0; i < t.n_tiles && ok; ++i) {
-                    const uint32_t n = done + i, next = n + 1;
-                    const int stage = n % AS_STAGES;
-                    ok = wait(&sh.v_full[stage], (n / AS_STAGES) & 1);
-                    for (int s = 0; s < t.streams && ok; ++s) {
-                        ok = wait(&sh.p_full[s], ((s ? done1 : done) + i) & 1);
-                        if (!ok) break;
-                        tc_fence_after();
-                        if (elect_one()) {
+                    for (int i = 0; i < t.n_tiles && ok; ++i) {
+                        const uint32_t n = done + i, next = n + 1;
+                        const int stage = n % AS_STAGES;
+                        const uint64_t v_d = desc_rows_along_k(v_s + stage * TILE);
+                        const bool more = i + 1 < t.n_tiles;
+                        ok = wait_alone(&sh.v_full[stage], (n / AS_STAGES) & 1);
+                        for (int s = 0; s < t.streams && ok; ++s) {
 #pragma unroll
-                            for (int k = 0; k < AS_TN / 16; ++k)
-                                umma_bf16_ts_into(tmem + s * 256 + 128, tmem + s * 256 + k * 8, desc_rows_along_k(v_s + stage * TILE + k * 2048), id_o,
-                                                  i > 0 || k > 0);
-                            if (i + 1 == t.n_tiles) umma_commit(smem_u32(&sh.o_full[s]));
-                        }
-                        __syncwarp();
-                        if (i + 1 < t.n_tiles) {
-                            if (s == 0) {
-                                ok = wait(&sh.k_full[next % AS_STAGES], (next / AS_STAGES) & 1);
+                            for (int half = 0; half < 2; ++half) {
+                                ok = ok && wait_alone(&sh.p_full[half][s], ((s ? done1 : done) + i) & 1);
+                                if (!ok) break;
                                 tc_fence_after();
+#pragma unroll
+                                for (int k = 0; k < AS_TN / 32; ++k) {
+                                    const int at = half * (AS_TN / 32) + k;
+                                    umma_bf16_ts_into(tmem + s * 256 + 128, tmem + s * 256 + at * 8, v_d + (at * 2048 >> 4), id_o, i > 0 || at > 0);
+                                }
                             }
-                            if (ok) scores(s, i + 1);
+                            if (!ok) break;
+                            if (!more) umma_commit(smem_u32(&sh.o_full[s]));
+                            else {
+                                if (s == 0) {
+                                    ok = wait_alone(&sh.k_full[next % AS_STAGES], (next / AS_STAGES) & 1);
+                                    tc_fence_after();
+                                }
+                                if (ok) scores(s, next);
+                            }
+                        }
+                        if (ok) {
+                            umma_commit(smem_u32(&sh.v_empty[stage]));
+                            if (more) umma_commit(smem_u32(&sh.k_empty[next % AS_STAGES]));
                         }
                     }
-                    if (ok && elect_one()) {
-                        umma_commit(smem_u32(&sh.v_empty[stage]));
-                        if (i + 1 < t.n_tiles) umma_commit(smem_u32(&sh.k_empty[next % AS_STAGES]));
-                    }
-                    __syncwarp();
                 }
+                __syncwarp();
             }
             end_unit(t);
         }
@@ -522,9 +573,11 @@ cudaError_t launch_attn_sm100(const AttnParams &p, int grid, cudaStream_t stream
     using Kernel = void (*)(const AttnParams, const CacheMaps);
     static const Kernel kernels[4] = {attn_sm100_kernel<64, false>, attn_sm100_kernel<64, true>, attn_sm100_kernel<128, false>, attn_sm100_kernel<128, true>};
     CacheMaps maps{};
-    maps.box = p.page_size < AS_TN ? p.page_size : AS_TN;
-    // (swizzled boxes begin on 1024 bytes, so that one has eight rows or more; strides that a tensor map cannot have are the other kernel's)
-    const bool tma = p.page_shift >= 3 && cache_map(&maps.k, p.k_cache, p, maps.box) && cache_map(&maps.v, p.v_cache, p, maps.box);
+    // a box is the largest power of two of tokens that divides a page and a tile, so that none crosses a page's end; swizzled boxes begin
+    // on 1024 bytes, so that one has eight rows or more; strides that a tensor map cannot have are the other kernel's
+    maps.box = p.page_size & -p.page_size;
+    if (maps.box > AS_TN) maps.box = AS_TN;
+    const bool tma = maps.box >= 8 && cache_map(&maps.k, p.k_cache, p, maps.box) && cache_map(&maps.v, p.v_cache, p, maps.box);
     const int which = (p.d == 128 ? 2 : 0) + (tma ? 1 : 0);
     const size_t smem = p.d == 128 ? as_smem<128>() : as_smem<64>();
     int sms = 0;
