@@ -64,7 +64,8 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
         const int row_first = g.m_tile * M, rows = min(M, g.s.rows * p.group - row_first);
         const int last_node = (row_first + rows - 1) / p.group, upto = p.row_offsets ? g.s.len + last_node + 1 : g.s.len;
         const int tile1 = min(g.tile1, max((upto + AR_TN - 1) / AR_TN, g.tile0));
-        const bool many = p.row_offsets && g.s.rows > 1;   // rows of the call that not all see
+        // tokens that all rows of the unit see: what lies behind them is hidden from some
+        const int common = !p.row_offsets ? upto : kind == AT_CHAIN ? g.s.len + row_first / p.group + 1 : g.s.len;
 
         // queries, through the last stage's place, to registers
         {
@@ -142,11 +143,11 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
             put_place(tile + 3, page_ahead);
             page_ahead = page_of(tile + 4);
             const uint32_t k_s = base + (tile % AR_STAGES) * ar_stage_bytes<D>(), v_s = k_s + AR_TN * D * 2;
-            const bool tail = (tile + 1) * AR_TN > g.s.len;   // has places that not every row sees
-            if (tail && many) {   // (0 times an infinite value is no number: the product gets a 0 there, the value is added at the end)
+            const bool tail = (tile + 1) * AR_TN > common;   // has places that not every row sees
+            if (tail && common < upto) {   // (0 times an infinite value is no number: the product gets a 0 there, the value is added at the end)
                 for (int i = tid; i < AR_TN * PIECES; i += AR_THREADS) {
                     const int r = i / PIECES, t = tile * AR_TN + r;
-                    if (t < g.s.len || t >= upto) continue;
+                    if (t < common || t >= upto) continue;
                     uint4 *at = reinterpret_cast<uint4 *>(ar_base + (v_s - base) + ar_at<D>(r, i % PIECES));
                     uint4 u = *at;
                     bool odd = false;
@@ -284,7 +285,7 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
             }
             const int u = row_first + r, node = u / p.group;
             if (odd)
-                for (int j = 0; j <= node; ++j) {
+                for (int j = common - g.s.len; j <= node; ++j) {
                     const int t = g.s.len + j;
                     if (t < g.tile0 * AR_TN || t >= tile1 * AR_TN || !attn_sees(p, kind, anc, g.s.row0, node, j)) continue;
                     const long long at = attn_token_offset(p, g.b, t, upto);

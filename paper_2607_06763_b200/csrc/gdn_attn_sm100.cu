@@ -65,7 +65,12 @@ __device__ __forceinline__ void umma_bf16_ts_into(uint32_t d_tmem, uint32_t a_tm
                    "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])              \
                  : "memory")
 
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// One arrival for a whole warp.  (An arrival per thread has the 128 of a stream one behind the other: 500 clocks.)
+__device__ __forceinline__ void mbar_arrive_warp(uint32_t bar, int lane)
+{
+    __syncwarp();
+    if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 __device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 
@@ -152,7 +157,7 @@ __device__ __forceinline__ float2 power_of_two_by_products(float2 x)
 struct Unit {
     AttnSegment g;
     int row_first, rows, upto, tile1, n_tiles, streams;
-    bool many;   // rows of the call that not all rows see
+    int common;   // tokens that all its rows see: what lies behind them is hidden from some
 };
 
 template <int D, bool TMA> __global__ void __launch_bounds__(AS_THREADS, 1)
@@ -168,18 +173,18 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
     const __nv_bfloat16 *k_cache = static_cast<const __nv_bfloat16 *>(p.k_cache), *v_cache = static_cast<const __nv_bfloat16 *>(p.v_cache);
 
     if (tid == 0) {
-        mbar_init(smem_u32(&sh.q_full), 256);
+        mbar_init(smem_u32(&sh.q_full), 8);
         for (int i = 0; i < AS_STAGES; ++i) {
-            mbar_init(smem_u32(&sh.k_full[i]), TMA ? 1 : 32);
-            mbar_init(smem_u32(&sh.v_full[i]), 32);
+            mbar_init(smem_u32(&sh.k_full[i]), 1);
+            mbar_init(smem_u32(&sh.v_full[i]), 1);
             mbar_init(smem_u32(&sh.v_landed[i]), 1);
             mbar_init(smem_u32(&sh.k_empty[i]), 1);
             mbar_init(smem_u32(&sh.v_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
-            mbar_init(smem_u32(&sh.p_full[0][i]), 128);
-            mbar_init(smem_u32(&sh.p_full[1][i]), 128);
+            mbar_init(smem_u32(&sh.p_full[0][i]), 4);
+            mbar_init(smem_u32(&sh.p_full[1][i]), 4);
             mbar_init(smem_u32(&sh.o_full[i]), 1);
         }
         sh.dead = 0;
@@ -227,7 +232,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
             t.upto = p.row_offsets ? t.g.s.len + last_node + 1 : t.g.s.len;
             t.tile1 = min(t.g.tile1, max((t.upto + AS_TN - 1) / AS_TN, t.g.tile0));
             t.n_tiles = t.tile1 - t.g.tile0;
-            t.many = p.row_offsets && t.g.s.rows > 1;
+            t.common = !p.row_offsets ? t.upto : kind == AT_CHAIN ? t.g.s.len + t.row_first / p.group + 1 : t.g.s.len;
             t.streams = t.rows > 128 ? 2 : 1;
             if (tid == 0) sh.odd = 0;
             __syncthreads();
@@ -259,7 +264,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                 for (int c = 0; c < PIECES; ++c) cp_async_16(q_s + stream * TILE + as_at(r & 127, c), src + c * 8, mine);
                 cp_async_wait_all();
                 fence_proxy_async();
-                mbar_arrive(smem_u32(&sh.q_full));
+                mbar_arrive_warp(smem_u32(&sh.q_full), lane);
             }
             if (stream < t.streams) {
                 const uint32_t seen_before = stream ? done1 : done;
@@ -274,7 +279,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) GDN_TMEM_LD32(s_at + c * 32, (x + c * 32));
                     tmem_wait_ld();
-                    bool hidden = (tile + 1) * AS_TN > g.s.len || stream * 128 + 128 > t.rows;   // from some row of this warp, some token
+                    bool hidden = (tile + 1) * AS_TN > t.common || stream * 128 + 128 > t.rows;   // from some row of this warp, some token
                     if (hidden) {
                         uint32_t see[4], all = ~0u;   // bit j: this row sees token tile * AS_TN + 32 c + j
 #pragma unroll
@@ -337,7 +342,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         if (c == 1 || c == 3) {   // half of the tile's weights: their part of the second product may begin
                             tmem_wait_st();
                             tc_fence_before();
-                            mbar_arrive(smem_u32(&sh.p_full[c >> 1][stream]));
+                            mbar_arrive_warp(smem_u32(&sh.p_full[c >> 1][stream]), lane);
                         }
                     }
                     l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
@@ -360,7 +365,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                             for (int j = 0; j < 32; ++j) x[j] = 0;
                         }
                         if (odd && mine)
-                            for (int j = 0; j <= node; ++j) {
+                            for (int j = t.common - g.s.len; j <= node; ++j) {
                                 const int at_token = g.s.len + j;
                                 if (at_token < g.tile0 * AS_TN || at_token >= t.tile1 * AS_TN || !attn_sees(p, kind, sh.anc, g.s.row0, node, j)) continue;
                                 const long long at = attn_token_offset(p, g.b, at_token, t.upto);
@@ -461,12 +466,12 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         cp_async_wait_all();
                         __syncwarp();
                     }
-                    // values of places that hold no token: zeros (their weights are 0, and 0 times what lies there may be no number); of rows of
-                    // the call that not every row sees: what is infinite or no number is taken out, and added at the end of the unit
-                    if (!keys && (tile + 1) * AS_TN > (t.many ? g.s.len : t.upto)) {
+                    // values of places that hold no token: zeros (their weights are 0, and 0 times what lies there may be no number); of tokens that
+                    // not every row sees: what is infinite or no number is taken out, and added at the end of the unit
+                    if (!keys && (tile + 1) * AS_TN > t.common) {
                         for (int k = lane; k < AS_TN * PIECES; k += 32) {
                             const int row = k / PIECES, token = tile * AS_TN + row;
-                            if (token < g.s.len && token < t.upto) continue;
+                            if (token < t.common) continue;
                             uint4 *at = reinterpret_cast<uint4 *>(data + (v_s - q_s) + stage * TILE + as_at(row, k % PIECES));
                             uint4 y = *at;
                             if (token >= t.upto) *at = make_uint4(0, 0, 0, 0);
@@ -479,7 +484,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                     }
                     if (!TMA || !keys) {
                         fence_proxy_async();
-                        mbar_arrive(smem_u32(&full[stage]));
+                        mbar_arrive_warp(smem_u32(&full[stage]), lane);
                     }
                 }
             } else if (warp == 10 && t.n_tiles > 0) {   // ---- products, by one thread: what it does between two of them the tensor cores may wait for
