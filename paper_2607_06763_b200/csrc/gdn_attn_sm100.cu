@@ -279,11 +279,11 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) GDN_TMEM_LD32(s_at + c * 32, (x + c * 32));
                     tmem_wait_ld();
-                    bool hidden = (tile + 1) * AS_TN > t.common || stream * 128 + 128 > t.rows;   // from some row of this warp, some token
+                    bool hidden = (tile + 1) * AS_TN > t.common;   // from some row of this warp, some token
                     if (hidden) {
                         uint32_t see[4], all = ~0u;   // bit j: this row sees token tile * AS_TN + 32 c + j
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) all &= see[c] = mine ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : 0;
+                        for (int c = 0; c < 4; ++c) all &= see[c] = mine ? seen_word(p, kind, sh.anc, g.s, node, tile * AS_TN + c * 32) : ~0u;   // (no row: zeros, written nowhere)
                         hidden = __any_sync(0xffffffffu, all != ~0u);
                         if (hidden) {
 #pragma unroll
