@@ -6,13 +6,17 @@
 // kept weights exceeds u * (their sum).
 //
 // A row is read once: the CTAs of a cluster (one to eight) hold it in shared memory and go over it there.  Nothing is sorted but the
-// members of one bin: (m - x) / T in units of 1/32 is a bin number that falls as x rises, one pass sums counts and weights
-// per bin, the bins' sums say in which bin a prefix ends, and only that bin's members (some hundreds of 131071) are put in order.
-// A bin with more members than fit (many equal logits) is bisected instead.
+// members of one bin: (m - x) / T in units of 1/32 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
+// The first k end in a bin that the counts tell.  Where the p end the counts nearly tell: a count times the weight at the bin's middle
+// is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, inside it and
+// altogether, and sees whether it is the one (else the estimate starts again from these sums).  Only that bin's members (some hundreds
+// of 131071) are put in order; a bin with more members than fit (many equal logits) is bisected instead.  What the pass summed up
+// to the bin, warp by warp, also says where the token lies.
 //
-// A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-40 (no order
-// of additions matters), and formed to about 1e-9 of themselves: fp32 steps on a difference m - x that is kept in two parts.  Tokens
-// more than 28 nats below the top weigh less than half a unit, and nothing.
+// A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-38 (no order
+// of additions matters).  Those of 2^-6 and more are formed to about 1e-9 of themselves, the others to fp32: their errors are as often
+// up as down, and 2^-30 at most.  The difference m - x is kept in two parts, and so is 1 / T.  Tokens more than 39 powers of two
+// below the top weigh less than a unit, and nothing.
 #include <cooperative_groups.h>
 
 #include "gdn_attn.cuh"
@@ -25,57 +29,129 @@ namespace gdn {
 namespace {
 
 constexpr int SA_THREADS = 512, SA_WARPS = SA_THREADS / 32;
-constexpr int SA_BINS = 1024;           // the last one: everything that weighs nothing
+constexpr int SA_BINS = 1024;           // two per thread
 constexpr float SA_PER_NAT = 32.f;
-constexpr int SA_SORT = 2048;           // members of a bin that are sorted
-constexpr int SA_UNIT = 40;             // weights in units of 2^-40
+constexpr int SA_SORT = 1024;           // members of a bin that are sorted
+constexpr int SA_UNIT = 38;             // weights in units of 2^-38
+constexpr float SA_COARSE = 6.f;        // weights below 2^-6 are formed to fp32
+constexpr float SA_LAST = 42.f;         // a weight of 2^-42 is none
 typedef unsigned long long u64;
 
+// 2^(38 - j/32), rounded.
+__constant__ u64 powers[32] = {
+    274877906944ull, 268987840221ull, 263223985481ull, 257583638263ull,
+    252064152055ull, 246662937055ull, 241377458955ull, 236205237751ull,
+    231143846582ull, 226190910588ull, 221344105800ull, 216601158044ull,
+    211959841877ull, 207417979546ull, 202973439958ull, 198624137689ull,
+    194368031998ull, 190203125877ull, 186127465105ull, 182139137339ull,
+    178236271212ull, 174417035459ull, 170679638052ull, 167022325365ull,
+    163443381347ull, 159941126720ull, 156513918187ull, 153160147665ull,
+    149878241531ull, 146666659877ull, 143523895795ull, 140448474667ull};
+
 struct SampleShared {
-    u64 table[32];                      // 2^(-j/32) in units
-    u64 sorted[SA_SORT];
-    float table_16[32];                 // the same in units of 16
-    u64 mass[SA_BINS];                  // of the CTA; then, for the bins of this rank's share, of the cluster
-    uint32_t count[SA_BINS];
-    u64 sum[2][SA_WARPS + 1];           // of the CTA's warps, then of the CTA (read by the cluster), in turn
-    uint32_t number[2][SA_WARPS + 1];
+    u64 table[32];                      // `powers`
+    float table_4[32];                  // the same in units of 4
+    u64 sorted[SA_SORT];                // rank 0: members of a bin
+    uint32_t count[SA_BINS];            // of the CTA; then, for the bins of this rank's share, of the cluster
+    u64 sum[2][3][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
     float top[SA_WARPS + 1];
+    int best[SA_WARPS + 1];
     int members;                        // rank 0: entries of `sorted`
-    u64 cut_key, cut_mass;              // rank 0: where a prefix ends inside a bin, and what it weighs up to there
+    u64 cut_key;                        // rank 0: where a prefix ends inside a bin
     uint32_t scan_n[SA_WARPS];
-    u64 scan_w[SA_WARPS];
-    int bin;                            // where a prefix ends
+    float scan_a[SA_WARPS];
+    int bin;
     uint32_t before_n;
-    u64 before_w;
-    int picked;
 };
 
-// In units, of the token whose logit is d + lo below the top; per = 32 log2(e) / T in two parts.
+__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return make_float2(a.x - b.x, a.y - b.y); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
+        "mov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Weights in units of tokens with given logits; per = log2(e) / T in two parts.
 struct Weigh {
-    float m, per_hi, per_lo;
+    float m, per_hi, per_lo, d_coarse, d_last;   // differences from the top: where fp32 does, where nothing is left
     bool finite;
     const u64 *table;
-    const float *table_16;
-    __device__ __forceinline__ u64 operator()(float x) const
+    const float *table_4;
+
+    // To about 1e-9, whatever the size.
+    __device__ __forceinline__ u64 fine(float x) const
     {
+        if (!finite) return x == m ? 1ull << SA_UNIT : 0;
         const float d = fmaxf(m - x, 0.f);
-        const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
-        if (!(t < 28.f * 1.4426950408889634f * 32.f && d < INFINITY)) return 0;
+        if (!(d < d_last)) return 0;
         // m - x = d + lo exactly
-        const float back = d - m;
-        const float lo = finite ? (m - (d - back)) + (-x - back) : 0.f;
-        const float err = fmaf(d, per_hi, -t) + fmaf(d, per_lo, lo * per_hi);
-        const float shifted = t + 12582912.f;               // 1.5 * 2^23: rounds t to a whole number
+        const float back = d - m, lo = (m - (d - back)) + (-x - back);
+        const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
+        const float err = fmaf(lo, per_hi, fmaf(d, per_hi, -t) + d * per_lo);
+        const float t32 = t * 32.f;
+        const float shifted = t32 + 12582912.f;                 // 1.5 * 2^23: rounds to a whole number
         const int n = __float_as_int(shifted) - 0x4B400000;
-        const float r = -((t - (shifted - 12582912.f)) + err) * 0.021660849392498290f;   // ln(2) / 32
+        const float r = -((t32 - (shifted - 12582912.f)) + 32.f * err) * 0.021660849392498290f;   // ln(2) / 32
         // e^r - 1 of |r| <= 0.011: the terms of its series
         const float q = r * fmaf(r, fmaf(r, fmaf(r, 0.041666666666666664f, 0.16666666666666666f), 0.5f), 1.f);
-        const u64 w = table[n & 31];
-        // (the correction is below 2^40 * 0.011 < 2^34: in units of 16 it fits a 32-bit number)
-        const long long c = (long long)__float2int_rn(table_16[n & 31] * q) * 16;
-        const u64 v = w + (u64)c;
+        // (the correction is below 2^38 * 0.011 < 2^32: in units of 4 it fits a 32-bit number)
+        const u64 v = table[n & 31] + (u64)((long long)__float2int_rn(table_4[n & 31] * q) * 4);
         const int down = n >> 5;
         return down ? (v + (1ull << (down - 1))) >> down : v;
+    }
+    // Two at a time, to fp32 (below 2^32 units: of tokens behind d_coarse; of the others something).
+    __device__ __forceinline__ void coarse(float2 x, uint32_t &w0, uint32_t &w1) const
+    {
+        const float2 mm = both(m), hi = both(per_hi);
+        float2 d = sub2(mm, x);
+        const float2 lo = sub2(sub2(mm, d), x);                 // what the difference loses, where |x| <= m
+        d.x = fminf(fmaxf(d.x, d_coarse), d_last);
+        d.y = fminf(fmaxf(d.y, d_coarse), d_last);
+        const float2 t = make_float2(__fmul_rn(d.x, -per_hi), __fmul_rn(d.y, -per_hi));
+        float2 e = fma2(d, hi, t);
+        e = fma2(d, both(per_lo), e);
+        e.x = d.x < d_last ? fmaf(lo.x, per_hi, e.x) : 0.f;     // (no number where x is infinite)
+        e.y = d.y < d_last ? fmaf(lo.y, per_hi, e.y) : 0.f;
+        const float2 n = make_float2(__fadd_rn(t.x, 12582912.f), __fadd_rn(t.y, 12582912.f));
+        const float2 r = sub2(sub2(t, make_float2(__fadd_rn(n.x, -12582912.f), __fadd_rn(n.y, -12582912.f))), e);
+        // 2^r on [-1/2, 1/2]: the polynomial of degree 6 with the least relative error, 2e-9 (fitted to 2^r), to fp32
+        float2 q = fma2(r, both(0.0001534581242594868f), both(0.0013399930903688073f));
+        q = fma2(r, q, both(0.009618489071726799f));
+        q = fma2(r, q, both(0.05550328642129898f));
+        q = fma2(r, q, both(0.24022646248340607f));
+        q = fma2(r, q, both(0.6931471824645996f));
+        q = fma2(r, q, both(1.f));
+        w0 = __float2uint_rn(__int_as_float(__float_as_int(q.x) + ((__float_as_int(n.x) + (SA_UNIT - 0x4B400000)) << 23)));
+        w1 = __float2uint_rn(__int_as_float(__float_as_int(q.y) + ((__float_as_int(n.y) + (SA_UNIT - 0x4B400000)) << 23)));
+    }
+    __device__ __forceinline__ void four(const float4 &x, u64 (&w)[4]) const
+    {
+        if (!finite) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = fine((&x.x)[j]);
+            return;
+        }
+        uint32_t c[4];
+        coarse(make_float2(x.x, x.y), c[0], c[1]);
+        coarse(make_float2(x.z, x.w), c[2], c[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = c[j];
+        const float top = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w));
+        if (m - top < d_coarse) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (m - (&x.x)[j] < d_coarse) w[j] = fine((&x.x)[j]);
+        }
+    }
+    // Of a token that weighs something, in units, not rounded to one.
+    __device__ double exactly(float x) const
+    {
+        return finite ? exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453) * (double)(1ull << SA_UNIT)
+                      : (double)(1ull << SA_UNIT);
     }
 };
 
@@ -104,11 +180,11 @@ template <> struct Quad<__nv_bfloat16> {
     }
 };
 
-template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kernel(const SampleParams p, int chunk, int places)
+template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_kernel(const SampleParams p, int chunk, int places)
 {
     extern __shared__ __align__(16) unsigned char sa_smem[];
     SampleShared &sh = *reinterpret_cast<SampleShared *>(sa_smem);
-    T *x_s = reinterpret_cast<T *>(sa_smem + (sizeof(SampleShared) + 15) / 16 * 16);   // [places], a multiple of 128 per warp
+    T *x_s = reinterpret_cast<T *>(sa_smem + (sizeof(SampleShared) + 15) / 16 * 16);   // [places], a multiple of 8 per warp
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -116,10 +192,11 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
     constexpr int PIECE = 16 / (int)sizeof(T);
 
     if (tid < 32) {
-        const double w = exp2((double)SA_UNIT - tid / 32.0);
-        sh.table[tid] = (u64)(w + 0.5);
-        sh.table_16[tid] = (float)(w / 16.0);
+        sh.table[tid] = powers[tid];
+        sh.table_4[tid] = (float)powers[tid] * 0.25f;
     }
+    if (tid == 0) sh.members = 0;
+    for (int i = tid; i < SA_BINS; i += SA_THREADS) sh.count[i] = 0;
     wait_for_previous_kernel();
 
     // ---- the row's part [first, first + n) of this CTA, at places shift ... of x_s: 16-byte pieces of both line up
@@ -167,11 +244,6 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     if (lane == 0) sh.top[warp] = top;
-    for (int i = tid; i < SA_BINS; i += SA_THREADS) {
-        sh.count[i] = 0;
-        sh.mass[i] = 0;
-    }
-    if (tid == 0) sh.members = 0;
     __syncthreads();
     if (tid < 32) {
         float t = lane < SA_WARPS ? sh.top[lane] : -INFINITY;
@@ -185,62 +257,14 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
 
     const float T_row = p.temperature ? p.temperature[row] : 1.f;
     const bool greedy = !(T_row > 0.f);
-    int k = p.top_k ? p.top_k[row] : 0;
-    if (k >= p.vocab) k = 0;
-    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
-    const bool by_k = k > 0, by_p = top_p < 1.f;
-    const double per = fmin(32.0 * 1.4426950408889634 / (double)T_row, 1e30);
-    const Weigh weigh{m, (float)per, (float)(per - (double)(float)per), m < INFINITY, sh.table, sh.table_16};
-    const float to_bin = (float)fmin((double)SA_PER_NAT / (double)T_row, 1e30);
-    auto place_of = [&](float x) { return fmaxf(m - x, 0.f) * to_bin; };   // its whole part is the bin (no number: the last)
-
-    // every four logits of the CTA's part, in rising order for one warp: a warp has `places / SA_WARPS` places
-    const int per_warp = places / SA_WARPS, from_place = warp * per_warp;
+    // a warp goes over its share of the places, four neighbouring ones per lane
+    const int from_place = warp * (places / SA_WARPS), to_place = from_place + places / SA_WARPS;
     auto index_at = [&](int place) { return first + place - shift; };
-    int turn = 0;
-    // sums over the cluster of (w, c) of all threads; before_w: of the ranks and warps in front of this warp
-    auto cluster_sum = [&](u64 w, uint32_t c, u64 &all_w, uint32_t &all_c, u64 *before_w) {
-#pragma unroll
-        for (int off = 16; off; off >>= 1) {
-            w += __shfl_xor_sync(0xffffffffu, w, off);
-            c += __shfl_xor_sync(0xffffffffu, c, off);
-        }
-        if (lane == 0) {
-            sh.sum[turn][warp] = w;
-            sh.number[turn][warp] = c;
-        }
-        __syncthreads();
-        if (tid == 0) {
-            u64 a = 0;
-            uint32_t b = 0;
-            for (int i = 0; i < SA_WARPS; ++i) {
-                a += sh.sum[turn][i];
-                b += sh.number[turn][i];
-            }
-            sh.sum[turn][SA_WARPS] = a;
-            sh.number[turn][SA_WARPS] = b;
-        }
-        cluster.sync();
-        all_w = 0;
-        all_c = 0;
-        u64 front = 0;
-        for (int r = 0; r < ranks; ++r) {
-            const u64 a = *cluster.map_shared_rank(&sh.sum[turn][SA_WARPS], r);
-            if (r < rank) front += a;
-            all_w += a;
-            all_c += *cluster.map_shared_rank(&sh.number[turn][SA_WARPS], r);
-        }
-        if (before_w) {
-            for (int i = 0; i < warp; ++i) front += sh.sum[turn][i];
-            *before_w = front;
-        }
-        turn ^= 1;   // (the next sum's barrier lies between these reads and the sum after it)
-    };
 
     if (m == -INFINITY || greedy) {   // nothing to choose from, or the first of the largest
         int best = 0x7fffffff;
-        if (m > -INFINITY)
-            for (int i = from_place + lane * 4; i < from_place + per_warp; i += 128) {
+        if (m > -INFINITY && sh.top[SA_WARPS] == m)
+            for (int i = from_place + lane * 4; i < to_place; i += 128) {
                 const float4 v = Quad<T>::get(x_s + i);
 #pragma unroll
                 for (int j = 3; j >= 0; --j)
@@ -248,15 +272,15 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
             }
 #pragma unroll
         for (int off = 16; off; off >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, off));
-        if (lane == 0) sh.number[0][warp] = (uint32_t)best;
+        if (lane == 0) sh.best[warp] = best;
         __syncthreads();
         if (tid == 0) {
-            for (int i = 0; i < SA_WARPS; ++i) best = min(best, (int)sh.number[0][i]);
-            sh.number[0][SA_WARPS] = (uint32_t)best;
+            for (int i = 0; i < SA_WARPS; ++i) best = min(best, sh.best[i]);
+            sh.best[SA_WARPS] = best;
         }
         cluster.sync();
         if (rank == 0 && tid == 0) {
-            for (int r = 0; r < ranks; ++r) best = min(best, (int)*cluster.map_shared_rank(&sh.number[0][SA_WARPS], r));
+            for (int r = 0; r < ranks; ++r) best = min(best, *cluster.map_shared_rank(&sh.best[SA_WARPS], r));
             p.token[row] = m > -INFINITY ? best : -1;
             if (p.prob) p.prob[row] = m > -INFINITY ? 1.f : 0.f;
         }
@@ -264,93 +288,103 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
         return;
     }
 
+    int k = p.top_k ? p.top_k[row] : 0;
+    if (k >= p.vocab) k = 0;
+    const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
+    const bool by_k = k > 0, by_p = top_p < 1.f;
+    const double per = fmin(1.4426950408889634 / (double)T_row, 1e30);
+    const float per_hi = (float)per, per_lo = (float)(per - (double)per_hi);
+    // (differences where per rounds to 0 are unbounded; a little inside SA_COARSE and SA_LAST whatever the quotients' rounding)
+    const Weigh weigh{m, per_hi, per_lo, fminf(SA_COARSE * 1.000001f / per_hi, 3e38f), fminf(SA_LAST / per_hi, 3e38f), m < INFINITY, sh.table, sh.table_4};
+    const float to_bin = (float)fmin((double)SA_PER_NAT / (double)T_row, 1e30);
+    auto place_of = [&](float x) { return fmaxf(m - x, 0.f) * to_bin; };   // its whole part is the bin
+
+    int turn = 0;
+    // sums of three numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
+    auto cluster_sum = [&](u64 (&a)[3], u64 (&all)[3], u64 *before) {
+#pragma unroll
+        for (int off = 16; off; off >>= 1)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) a[i] += __shfl_xor_sync(0xffffffffu, a[i], off);
+        if (lane < 3) sh.sum[turn][lane][warp] = lane == 0 ? a[0] : lane == 1 ? a[1] : a[2];
+        __syncthreads();
+        if (tid < 3) {
+            u64 s = 0;
+            for (int i = 0; i < SA_WARPS; ++i) s += sh.sum[turn][tid][i];
+            sh.sum[turn][tid][SA_WARPS] = s;
+        }
+        cluster.sync();
+        u64 front = 0;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) all[i] = 0;
+        for (int r = 0; r < ranks; ++r) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) all[i] += *cluster.map_shared_rank(&sh.sum[turn][i][SA_WARPS], r);
+            if (before && r + 1 == rank) front = all[0];
+        }
+        if (before) {
+            for (int i = 0; i < warp; ++i) front += sh.sum[turn][0][i];
+            *before = front;
+        }
+        turn ^= 1;   // (the next sum's barrier lies between these reads and the sum after it)
+    };
+
     // ---- where the kept prefix ends: tokens of bins in front of `cut_bin`, and of that bin those with keys up to `cut_key`
-    int cut_bin = SA_BINS - 1;
+    int cut_bin = SA_BINS;
     u64 cut_key = ~0ull;
+    auto inside = [&](float b, float x, int place) {   // of the prefix
+        return b < (float)cut_bin || (b < (float)(cut_bin + 1) && key_of(x, index_at(place)) <= cut_key);
+    };
+    const u64 least = min_p > 0.f ? (u64)ceil(fmin((double)min_p, 1.0) * (double)(1ull << SA_UNIT)) : 0;
+    u64 w = 0;              // this thread's share of the kept weights
+    bool summed = false;    // where it is known already
     if (by_k || by_p) {
-        for (int i = from_place + lane * 4; i < from_place + per_warp; i += 128) {
+        for (int i = from_place + lane * 4; i < to_place; i += 128) {
             const float4 v = Quad<T>::get(x_s + i);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float x = (&v.x)[j], b = place_of(x);
-                if (b < (float)(SA_BINS - 1)) {
-                    if (by_k) atomicAdd(&sh.count[(int)b], 1u);
-                    if (by_p) atomicAdd(&sh.mass[(int)b], weigh(x));
-                }
+                const float b = place_of((&v.x)[j]);
+                if (b < (float)SA_BINS) atomicAdd(&sh.count[(int)b], 1u);
             }
         }
-        // bins' sums over the cluster: each rank those of its share, then everybody reads all of them
         cluster.sync();
+        // bins' counts over the cluster: each rank those of its share, then everybody reads all of them
         const int share = SA_BINS / ranks;
         for (int i = rank * share + tid; i < (rank + 1) * share; i += SA_THREADS) {
             uint32_t c = 0;
-            u64 w = 0;
-            for (int r = 0; r < ranks; ++r) {
-                if (by_k) c += *cluster.map_shared_rank(&sh.count[i], r);
-                if (by_p) w += *cluster.map_shared_rank(&sh.mass[i], r);
-            }
+            for (int r = 0; r < ranks; ++r) c += *cluster.map_shared_rank(&sh.count[i], r);
             sh.count[i] = c;   // (of this bin no other rank reads this copy)
-            sh.mass[i] = w;
         }
         cluster.sync();
-        // this thread's two bins, and the sums over all in front of them
-        uint32_t c2[2], cb;
-        u64 w2[2], wb;
+        uint32_t c2[2], cb;    // this thread's two bins, and the counts of all in front of them
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int i = 2 * tid + j;
-            c2[j] = *cluster.map_shared_rank(&sh.count[i], i / share);
-            w2[j] = *cluster.map_shared_rank(&sh.mass[i], i / share);
-        }
+        for (int j = 0; j < 2; ++j) c2[j] = *cluster.map_shared_rank(&sh.count[2 * tid + j], (2 * tid + j) / share);
         {
             uint32_t c = c2[0] + c2[1];
-            u64 w = w2[0] + w2[1];
-            const uint32_t c_own = c;
-            const u64 w_own = w;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
-                const uint32_t cu = __shfl_up_sync(0xffffffffu, c, off);
-                const u64 wu = __shfl_up_sync(0xffffffffu, w, off);
-                if (lane >= off) {
-                    c += cu;
-                    w += wu;
-                }
+                const uint32_t up = __shfl_up_sync(0xffffffffu, c, off);
+                if (lane >= off) c += up;
             }
-            if (lane == 31) {
-                sh.scan_n[warp] = c;
-                sh.scan_w[warp] = w;
-            }
+            if (lane == 31) sh.scan_n[warp] = c;
+            if (tid == 0) sh.bin = SA_BINS;
             __syncthreads();
-            cb = c - c_own;
-            wb = w - w_own;
-            for (int i = 0; i < warp; ++i) {
-                cb += sh.scan_n[i];
-                wb += sh.scan_w[i];
-            }
+            cb = c - c2[0] - c2[1];
+            for (int i = 0; i < warp; ++i) cb += sh.scan_n[i];
         }
-        u64 z = 0;   // weight of the first k (all, where k is off)
-        for (int i = 0; i < SA_WARPS; ++i) z += sh.scan_w[i];
-
-        // The end of a prefix inside bin `bin`: the smallest key there up to which `enough` holds of the (count, weight) of the
-        // bin's members with keys up to it; and that weight.
-        auto end_in_bin = [&](int bin, auto enough, u64 &key, u64 &weight) {
-            auto in_bin = [&](float x) {
-                const float b = place_of(x);
-                return b >= (float)bin && b < (float)(bin + 1);
-            };
-            int *members = cluster.map_shared_rank(&sh.members, 0);
-            u64 *list = cluster.map_shared_rank(sh.sorted, 0);
-            for (int i = from_place + lane * 4; i < from_place + per_warp; i += 128) {
-                const float4 v = Quad<T>::get(x_s + i);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (in_bin((&v.x)[j])) {
-                        const int at = atomicAdd(members, 1);
-                        if (at < SA_SORT) list[at] = key_of((&v.x)[j], index_at(i + j));
-                    }
+        auto in_bin = [&](float b, int bin) { return b >= (float)bin && b < (float)(bin + 1); };
+        // the members of a bin, those of the prefix so far, to rank 0's list
+        auto gather = [&](float b, float x, int place, int bin) {
+            if (in_bin(b, bin) && inside(b, x, place)) {
+                const int at = atomicAdd(cluster.map_shared_rank(&sh.members, 0), 1);
+                if (at < SA_SORT) cluster.map_shared_rank(sh.sorted, 0)[at] = key_of(x, index_at(place));
             }
-            cluster.sync();
-            const int have = *members;
+        };
+        // The smallest key of the bin's members in the list up to which `enough` holds of the (count, weight) of those with keys up to it;
+        // where they were too many for the list, found bit by bit, each with a pass over the row.  After a barrier of the cluster.
+        auto end_in_list = [&](int bin, bool weights, auto enough) {
+            const int have = *cluster.map_shared_rank(&sh.members, 0);
+            u64 key = ~0ull;
             if (have <= SA_SORT) {
                 if (rank == 0) {   // in order by exchanges at distances that are powers of two
                     int size = 32;
@@ -376,153 +410,268 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS) sample_kerne
                         for (int i = 0; i < have && !found; i += 32) {
                             const bool there = i + lane < have;
                             const u64 own_key = sh.sorted[min(i + lane, have - 1)];
-                            u64 w = there ? weigh(logit_of(own_key)) : 0;
+                            u64 upto = there && weights ? weigh.fine(logit_of(own_key)) : 0;
 #pragma unroll
                             for (int off = 1; off < 32; off <<= 1) {
-                                const u64 up = __shfl_up_sync(0xffffffffu, w, off);
-                                if (lane >= off) w += up;
+                                const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
+                                if (lane >= off) upto += up;
                             }
-                            const unsigned yes = __ballot_sync(0xffffffffu, there && enough((uint32_t)(i + lane + 1), sum + w));
+                            const unsigned yes = __ballot_sync(0xffffffffu, there && enough((uint32_t)(i + lane + 1), sum + upto));
                             const int at = yes ? __ffs(yes) - 1 : min(31, have - 1 - i);
-                            const u64 upto = sum + __shfl_sync(0xffffffffu, w, at), k_at = __shfl_sync(0xffffffffu, own_key, at);
+                            const u64 k_at = __shfl_sync(0xffffffffu, own_key, at);
                             found = yes != 0;
-                            if (lane == 0) {
-                                sh.cut_key = k_at;
-                                sh.cut_mass = upto;
-                            }
-                            sum += __shfl_sync(0xffffffffu, w, 31);
+                            if (lane == 0) sh.cut_key = k_at;
+                            sum += __shfl_sync(0xffffffffu, upto, 31);
                         }
                     }
                 }
                 cluster.sync();
-                if (rank == 0 && tid == 0) sh.members = 0;   // (everybody has read it)
                 key = *cluster.map_shared_rank(&sh.cut_key, 0);
-                weight = *cluster.map_shared_rank(&sh.cut_mass, 0);
-                cluster.sync();   // (before the list is used again)
-                return;
-            }
-            // too many of them: the key bit by bit, each with a pass over the row
-            key = ~0ull;
-            weight = 0;
-            u64 lo = 0, hi = ~0ull;
-            while (lo < hi) {
-                const u64 mid = lo + (hi - lo) / 2;
-                u64 w = 0, w_all;
-                uint32_t c = 0, c_all;
-                for (int i = from_place + lane * 4; i < from_place + per_warp; i += 128) {
-                    const float4 v = Quad<T>::get(x_s + i);
+            } else {
+                u64 lo = 0, hi = ~0ull;
+                while (lo < hi) {
+                    const u64 mid = lo + (hi - lo) / 2;
+                    u64 a[3] = {0, 0, 0}, all[3];
+                    for (int i = from_place + lane * 4; i < to_place; i += 128) {
+                        const float4 v = Quad<T>::get(x_s + i);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (in_bin((&v.x)[j]) && key_of((&v.x)[j], index_at(i + j)) <= mid) {
-                            ++c;
-                            w += weigh((&v.x)[j]);
+                        for (int j = 0; j < 4; ++j) {
+                            const float x = (&v.x)[j], b = place_of(x);
+                            if (in_bin(b, bin) && key_of(x, index_at(i + j)) <= mid && inside(b, x, i + j)) {
+                                ++a[1];
+                                if (weights) a[0] += weigh.fine(x);
+                            }
                         }
+                    }
+                    cluster_sum(a, all, nullptr);
+                    if (all[1] && enough((uint32_t)all[1], all[0])) hi = mid;
+                    else lo = mid + 1;
                 }
-                cluster_sum(w, c, w_all, c_all, nullptr);
-                if (c_all && enough(c_all, w_all)) {
-                    hi = mid;
-                    weight = w_all;
-                } else
-                    lo = mid + 1;
+                key = lo;
             }
-            key = lo;
+            return key;
+        };
+        auto empty_list = [&]() {
+            cluster.sync();   // (everybody has read it)
             if (rank == 0 && tid == 0) sh.members = 0;
             cluster.sync();
         };
-        // which bin: its sums are in one thread
-        auto end_in = [&](auto enough, u64 &weight) {
-            if (tid == 0) sh.bin = SA_BINS - 1;
-            __syncthreads();
+
+        if (by_k) {   // the bin in which the k-th token lies, and its key
             uint32_t c = cb;
-            u64 w = wb;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const bool was = (c > 0 || w > 0) && enough(c, w);   // (an empty prefix is never enough: one token is kept)
-                c += c2[j];
-                w += w2[j];
-                if (!was && (c2[j] || w2[j]) && enough(c, w)) {
+                if (c < (uint32_t)k && (uint32_t)k <= c + c2[j]) {
                     sh.bin = 2 * tid + j;
-                    sh.before_n = c - c2[j];
-                    sh.before_w = w - w2[j];
+                    sh.before_n = c;
                 }
+                c += c2[j];
             }
             __syncthreads();
             const int bin = sh.bin;
-            const uint32_t bn = sh.before_n;
-            const u64 bw = sh.before_w;
-            u64 key = ~0ull;
-            if (bin < SA_BINS - 1) {
-                u64 inside;
-                end_in_bin(bin, [&](uint32_t cc, u64 ww) { return enough(bn + cc, bw + ww); }, key, inside);
-                weight = bw + inside;
-            }
-            __syncthreads();
-            if (bin < cut_bin || (bin == cut_bin && key < cut_key)) {
+            if (bin < SA_BINS) {   // (else all that weigh anything are among the first k)
+                const uint32_t wanted = (uint32_t)k - sh.before_n;
+                for (int i = from_place + lane * 4; i < to_place; i += 128) {
+                    const float4 v = Quad<T>::get(x_s + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) gather(place_of((&v.x)[j]), (&v.x)[j], i + j, bin);
+                }
+                cluster.sync();
+                const u64 key = end_in_list(bin, false, [&](uint32_t cc, u64) { return cc >= wanted; });
+                empty_list();
                 cut_bin = bin;
                 cut_key = key;
             }
-        };
-        if (by_k) end_in([&](uint32_t c, u64) { return c >= (uint32_t)k; }, z);
+        }
         if (by_p) {
-            const double goal = (double)top_p * (double)z;
-            u64 unused = 0;
-            end_in([&](uint32_t, u64 w) { return (double)w >= goal; }, unused);
+            // weights by the counts, in units; of the prefix so far, whose last bin counts as far as it belongs to it
+            float a2[2], ab;
+            {
+                uint32_t c = cb;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int bin = 2 * tid + j;
+                    const float in = bin < cut_bin ? (float)c2[j] : bin == cut_bin ? (float)((uint32_t)k - c) : 0.f;
+                    a2[j] = in * exp2f((float)SA_UNIT - ((float)bin + 0.5f) * (1.4426950408889634f / SA_PER_NAT));
+                    c += c2[j];
+                }
+                float a = a2[0] + a2[1];
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const float up = __shfl_up_sync(0xffffffffu, a, off);
+                    if (lane >= off) a += up;
+                }
+                if (lane == 31) sh.scan_a[warp] = a;
+                __syncthreads();
+                ab = a - a2[0] - a2[1];
+                for (int i = 0; i < warp; ++i) ab += sh.scan_a[i];
+            }
+            float estimate = 0.f;   // of everything
+            for (int i = 0; i < SA_WARPS; ++i) estimate += sh.scan_a[i];
+            // the first bin in (from, to) that has members of the prefix and up to whose end about `goal` has gathered; else the last, or -1
+            auto search = [&](int from, int to, float goal) {
+                __syncthreads();
+                if (tid == 0) {
+                    sh.bin = SA_BINS;
+                    sh.best[0] = -1;
+                }
+                __syncthreads();
+                float a = ab;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int bin = 2 * tid + j;
+                    a += a2[j];
+                    if (bin > from && bin < to && c2[j] && bin <= cut_bin) {
+                        if (a >= goal) atomicMin(&sh.bin, bin);
+                        atomicMax(&sh.best[0], bin);
+                    }
+                }
+                __syncthreads();
+                return sh.bin < SA_BINS ? sh.bin : sh.best[0];
+            };
+            int low = -1, high = SA_BINS, bin = search(low, high, top_p * estimate);
+            bool found = false;
+            u64 up = 0, z = 0;
+            while (bin >= 0) {   // ends: the bins between low and high get fewer
+                u64 a[3] = {0, 0, 0}, all[3], keep = 0;   // up to the bin, inside it, all of the prefix
+                for (int i = from_place + lane * 4; i < to_place; i += 128) {
+                    const float4 v = Quad<T>::get(x_s + i);
+                    u64 w4[4];
+                    float b[4];
+                    bool any = false;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        b[j] = place_of((&v.x)[j]);
+                        any |= b[j] < (float)(cut_bin + 1);
+                    }
+                    if (!any) continue;
+                    weigh.four(v, w4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (by_k && !inside(b[j], (&v.x)[j], i + j)) continue;
+                        a[2] += w4[j];
+                        if (b[j] < (float)bin) {
+                            a[0] += w4[j];
+                            if (w4[j] >= least) keep += w4[j];
+                        } else if (b[j] < (float)(bin + 1)) {
+                            a[1] += w4[j];
+                            gather(b[j], (&v.x)[j], i + j, bin);
+                        }
+                    }
+                }
+                cluster_sum(a, all, nullptr);
+                up = all[0];
+                z = all[2];
+                const double goal = (double)top_p * (double)z;
+                if (up > 0 && (double)up >= goal) high = bin;                          // it ends in front of the bin
+                else if ((double)(up + all[1]) < goal) low = bin;                      // or behind it
+                else {
+                    found = true;
+                    w = keep;
+                    break;
+                }
+                empty_list();
+                // the estimate again, from the sums that are now known: the threads' prefix sums are compared with a goal that is moved
+                float at_bin = ab;
+                if (tid == bin / 2) {
+                    if (bin & 1) at_bin += a2[0];
+                    sh.scan_a[0] = at_bin;                                             // estimated up to the bin
+                    sh.scan_a[1] = bin & 1 ? a2[1] : a2[0];
+                }
+                __syncthreads();
+                const float moved = high == bin ? (float)(goal - (double)up) + sh.scan_a[0]
+                                                : (float)(goal - (double)(up + all[1])) + sh.scan_a[0] + sh.scan_a[1];
+                bin = search(low, high, moved);
+            }
+            if (found) {
+                const double goal = (double)top_p * (double)z;
+                const u64 key = end_in_list(bin, true, [&](uint32_t, u64 ww) { return (double)(up + ww) >= goal; });
+                const int have = *cluster.map_shared_rank(&sh.members, 0);
+                cut_bin = bin;
+                cut_key = key;
+                summed = have <= SA_SORT;
+                if (!summed) w = 0;
+                else {   // the kept members of the bin that lie in this warp's share
+                    const u64 *list = cluster.map_shared_rank(sh.sorted, 0);
+                    for (int i = lane; i < have; i += 32) {
+                        const u64 member = list[i];
+                        const int index = (int)(uint32_t)member;
+                        if (member <= key && index >= index_at(from_place) && index < index_at(to_place) && index >= first && index < first + n) {
+                            const u64 ww = weigh.fine(logit_of(member));
+                            if (ww >= least) w += ww;
+                        }
+                    }
+                }
+            }
         }
     }
 
     // ---- the kept weights: of each warp, of the warps in front, of all
-    const u64 least = min_p > 0.f ? (u64)ceil(fmin((double)min_p, 1.0) * (double)(1ull << SA_UNIT)) : 0;
-    auto kept = [&](float x, int place) -> u64 {
-        const float b = place_of(x);
-        if (b < (float)cut_bin || (b < (float)(cut_bin + 1) && key_of(x, index_at(place)) <= cut_key)) {
-            const u64 w = weigh(x);
-            return w >= least ? w : 0;
-        }
-        return 0;
-    };
-    u64 w = 0, z, before;
-    uint32_t unused;
-    for (int i = from_place + lane * 4; i < from_place + per_warp; i += 128) {
-        const float4 v = Quad<T>::get(x_s + i);
+    auto kept_four = [&](const float4 &v, int place, u64 (&own)[4]) {
+        float b[4];
+        bool any = false;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w += kept((&v.x)[j], i + j);
-    }
-    cluster_sum(w, 0, z, unused, &before);
+        for (int j = 0; j < 4; ++j) {
+            own[j] = 0;
+            b[j] = place_of((&v.x)[j]);
+            any |= b[j] < (float)(cut_bin + 1);
+        }
+        if (!any) return;
+        u64 w4[4];
+        weigh.four(v, w4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (cut_bin < SA_BINS && !inside(b[j], (&v.x)[j], place + j)) continue;
+            // (members of the last bin are weighed as the list's are)
+            const u64 ww = cut_bin < SA_BINS && b[j] >= (float)cut_bin ? weigh.fine((&v.x)[j]) : w4[j];
+            own[j] = ww >= least ? ww : 0;
+        }
+    };
+    if (!summed)
+        for (int i = from_place + lane * 4; i < to_place; i += 128) {
+            u64 own[4];
+            kept_four(Quad<T>::get(x_s + i), i, own);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w += own[j];
+        }
+    u64 sums[3] = {w, 0, 0}, all[3], before;
+    cluster_sum(sums, all, &before);
+    const u64 z = all[0];
+    w = sums[0];   // of the warp
     double u = (double)p.uniform[row];
     u = u >= 0.0 ? u : 0.0;   // (no number: 0)
     const double at = u * (double)z;
     const u64 goal = at < (double)z ? min((u64)at, z - 1) : z - 1;
-#pragma unroll
-    for (int off = 16; off; off >>= 1) w += __shfl_xor_sync(0xffffffffu, w, off);
     if (before <= goal && goal < before + w) {   // this warp alone
         u64 sum = before;
-        for (int i = from_place; i < from_place + per_warp; i += 128) {
-            const float4 v = Quad<T>::get(x_s + i + lane * 4);
-            u64 own[4], four = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) four += own[j] = kept((&v.x)[j], i + lane * 4 + j);
+        for (int i = from_place; i < to_place; i += 128) {
+            u64 own[4] = {0, 0, 0, 0};
+            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            if (i + lane * 4 < to_place) {
+                v = Quad<T>::get(x_s + i + lane * 4);
+                kept_four(v, i + lane * 4, own);
+            }
+            const u64 four = own[0] + own[1] + own[2] + own[3];
             u64 upto = four;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
                 if (lane >= off) upto += up;
             }
-            const u64 all = __shfl_sync(0xffffffffu, upto, 31);
-            if (goal < sum + all) {
+            const u64 quads = __shfl_sync(0xffffffffu, upto, 31);
+            if (goal < sum + quads) {
                 u64 s = sum + upto - four;
-                bool mine = false;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (!mine && s <= goal && goal < s + own[j]) {
+                    if (s <= goal && goal < s + own[j]) {
                         p.token[row] = index_at(i + lane * 4 + j);
-                        if (p.prob) p.prob[row] = (float)((double)own[j] / (double)z);
-                        mine = true;
+                        if (p.prob) p.prob[row] = (float)(weigh.exactly((&v.x)[j]) / (double)z);
                     }
                     s += own[j];
                 }
                 break;
             }
-            sum += all;
+            sum += quads;
         }
     }
     cluster.sync();   // (nobody leaves while its shared memory is read)
@@ -536,7 +685,7 @@ cudaError_t launch_sample(const SampleParams &p, bool bf16, cudaStream_t stream)
     int ranks = 1;
     while (ranks < 8 && p.vocab > 4096 * ranks && (p.n_rows * ranks < 2 * 148 || p.vocab > 16384 * ranks)) ranks *= 2;
     const int chunk = ((p.vocab + ranks - 1) / ranks + 7) / 8 * 8;
-    const int step = 128 * SA_WARPS, places = (chunk + 8 + step - 1) / step * step;
+    const int step = 8 * SA_WARPS, places = (chunk + 8 + step - 1) / step * step;   // (up to seven in front of a row's part: 16-byte pieces)
     const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)places * (bf16 ? 2 : 4);
     static PerContext seen[2];
     const auto kernel = bf16 ? sample_kernel<__nv_bfloat16> : sample_kernel<float>;
