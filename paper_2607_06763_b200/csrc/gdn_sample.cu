@@ -5,7 +5,9 @@
 // gathered, Z_k the sum over the first k; those with w >= min_p.  The token is the first kept one, by index, at which the sum of
 // kept weights exceeds u * (their sum).
 //
-// A row is read once: the CTAs of a cluster (one to eight) hold it in shared memory and go over it there.  Nothing is sorted but the
+// A row belongs to the CTAs of a cluster (one to eight).  They go over it two to four times: from shared memory where a CTA's part is
+// small (few rows: what counts is the time of a pass), else from where the first reading left it, L2 (many rows: what counts is how
+// many CTAs an SM holds; the rows at work at one time are some 100 MB at most).  Nothing is sorted but the
 // members of one bin: (m - x) / T in units of 1/32 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
 // The first k end in a bin that the counts tell.  Where the p end the counts nearly tell: a count times the weight at the bin's middle
 // is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, inside it and
@@ -28,8 +30,9 @@ namespace gdn {
 
 namespace {
 
-constexpr int SA_THREADS = 512, SA_WARPS = SA_THREADS / 32;
-constexpr int SA_BINS = 1024;           // two per thread
+constexpr int SA_THREADS = 256, SA_WARPS = SA_THREADS / 32, SA_CTAS = 4;
+constexpr int SA_BINS = 1024, SA_OWN = SA_BINS / SA_THREADS;   // bins, of a thread
+constexpr int SA_HELD = 32 << 10;       // bytes of a row that a CTA holds in shared memory
 constexpr float SA_PER_NAT = 32.f;
 constexpr int SA_SORT = 1024;           // members of a bin that are sorted
 constexpr int SA_UNIT = 38;             // weights in units of 2^-38
@@ -64,30 +67,20 @@ struct SampleShared {
     uint32_t before_n;
 };
 
-__device__ __forceinline__ float2 sub2(float2 a, float2 b) { return make_float2(a.x - b.x, a.y - b.y); }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 d;
-    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\t"
-        "mov.b64 {%0, %1}, d;\n\t}"
-        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return d;
-}
-__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
-
 // Weights in units of tokens with given logits; per = log2(e) / T in two parts.
 struct Weigh {
-    float m, per_hi, per_lo, d_coarse, d_last;   // differences from the top: where fp32 does, where nothing is left
-    bool finite;
+    float m, per_hi, per_lo;
+    float x_fine, x_last;   // logits above the first are weighed finely; below the last nothing is left
+    bool all_fine;
     const u64 *table;
     const float *table_4;
 
     // To about 1e-9, whatever the size.
     __device__ __forceinline__ u64 fine(float x) const
     {
-        if (!finite) return x == m ? 1ull << SA_UNIT : 0;
-        const float d = fmaxf(m - x, 0.f);
-        if (!(d < d_last)) return 0;
+        if (x == m) return 1ull << SA_UNIT;
+        const float d = m - x;
+        if (!(d * per_hi < SA_LAST && d < INFINITY)) return 0;
         // m - x = d + lo exactly
         const float back = d - m, lo = (m - (d - back)) + (-x - back);
         const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
@@ -103,55 +96,44 @@ struct Weigh {
         const int down = n >> 5;
         return down ? (v + (1ull << (down - 1))) >> down : v;
     }
-    // Two at a time, to fp32 (below 2^32 units: of tokens behind d_coarse; of the others something).
-    __device__ __forceinline__ void coarse(float2 x, uint32_t &w0, uint32_t &w1) const
+    // To fp32, where x < x_fine (anything elsewhere).  (Two at a time by packed operations, each constant would take two registers.)
+    __device__ __forceinline__ uint32_t coarse(float x) const
     {
-        const float2 mm = both(m), hi = both(per_hi);
-        float2 d = sub2(mm, x);
-        const float2 lo = sub2(sub2(mm, d), x);                 // what the difference loses, where |x| <= m
-        d.x = fminf(fmaxf(d.x, d_coarse), d_last);
-        d.y = fminf(fmaxf(d.y, d_coarse), d_last);
-        const float2 t = make_float2(__fmul_rn(d.x, -per_hi), __fmul_rn(d.y, -per_hi));
-        float2 e = fma2(d, hi, t);
-        e = fma2(d, both(per_lo), e);
-        e.x = d.x < d_last ? fmaf(lo.x, per_hi, e.x) : 0.f;     // (no number where x is infinite)
-        e.y = d.y < d_last ? fmaf(lo.y, per_hi, e.y) : 0.f;
-        const float2 n = make_float2(__fadd_rn(t.x, 12582912.f), __fadd_rn(t.y, 12582912.f));
-        const float2 r = sub2(sub2(t, make_float2(__fadd_rn(n.x, -12582912.f), __fadd_rn(n.y, -12582912.f))), e);
+        x = fmaxf(x, x_last);   // (no number, too)
+        const float d = m - x;
+        const float lo = (m - d) - x;   // what the difference loses, where |x| <= m
+        const float t = __fmul_rn(d, -per_hi);
+        const float e = fmaf(lo, per_hi, fmaf(d, per_lo, fmaf(d, per_hi, t)));
+        const float n = t + 12582912.f;
+        const float r = (t - (n - 12582912.f)) - e;
         // 2^r on [-1/2, 1/2]: the polynomial of degree 6 with the least relative error, 2e-9 (fitted to 2^r), to fp32
-        float2 q = fma2(r, both(0.0001534581242594868f), both(0.0013399930903688073f));
-        q = fma2(r, q, both(0.009618489071726799f));
-        q = fma2(r, q, both(0.05550328642129898f));
-        q = fma2(r, q, both(0.24022646248340607f));
-        q = fma2(r, q, both(0.6931471824645996f));
-        q = fma2(r, q, both(1.f));
-        w0 = __float2uint_rn(__int_as_float(__float_as_int(q.x) + ((__float_as_int(n.x) + (SA_UNIT - 0x4B400000)) << 23)));
-        w1 = __float2uint_rn(__int_as_float(__float_as_int(q.y) + ((__float_as_int(n.y) + (SA_UNIT - 0x4B400000)) << 23)));
+        float q = fmaf(r, 0.0001534581242594868f, 0.0013399930903688073f);
+        q = fmaf(r, q, 0.009618489071726799f);
+        q = fmaf(r, q, 0.05550328642129898f);
+        q = fmaf(r, q, 0.24022646248340607f);
+        q = fmaf(r, q, 0.6931471824645996f);
+        q = fmaf(r, q, 1.f);
+        return __float2uint_rn(__int_as_float(__float_as_int(q) + (__float_as_int(n) << 23) + (SA_UNIT << 23)));   // (0x4B400000 << 23 is 0)
     }
     __device__ __forceinline__ void four(const float4 &x, u64 (&w)[4]) const
     {
-        if (!finite) {
+        if (all_fine) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = fine((&x.x)[j]);
             return;
         }
-        uint32_t c[4];
-        coarse(make_float2(x.x, x.y), c[0], c[1]);
-        coarse(make_float2(x.z, x.w), c[2], c[3]);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = c[j];
-        const float top = fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w));
-        if (m - top < d_coarse) {
+        for (int j = 0; j < 4; ++j) w[j] = coarse((&x.x)[j]);
+        if (fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) > x_fine) {
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (m - (&x.x)[j] < d_coarse) w[j] = fine((&x.x)[j]);
+                if ((&x.x)[j] > x_fine) w[j] = fine((&x.x)[j]);
         }
     }
     // Of a token that weighs something, in units, not rounded to one.
     __device__ double exactly(float x) const
     {
-        return finite ? exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453) * (double)(1ull << SA_UNIT)
-                      : (double)(1ull << SA_UNIT);
+        return (x == m ? 1.0 : exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453)) * (double)(1ull << SA_UNIT);
     }
 };
 
@@ -180,7 +162,7 @@ template <> struct Quad<__nv_bfloat16> {
     }
 };
 
-template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_kernel(const SampleParams p, int chunk, int places)
+template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, SA_CTAS) sample_kernel(const SampleParams p, int chunk, int places)
 {
     extern __shared__ __align__(16) unsigned char sa_smem[];
     SampleShared &sh = *reinterpret_cast<SampleShared *>(sa_smem);
@@ -199,47 +181,57 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
     for (int i = tid; i < SA_BINS; i += SA_THREADS) sh.count[i] = 0;
     wait_for_previous_kernel();
 
-    // ---- the row's part [first, first + n) of this CTA, at places shift ... of x_s: 16-byte pieces of both line up
+    // ---- the row's part [first, first + n) of this CTA, at places shift, shift + 1, ...: place 0 is on a 16-byte boundary
     const int first = min(rank * chunk, p.vocab), n = min(chunk, p.vocab - first);
     const T *src = static_cast<const T *>(p.logits) + (size_t)row * p.row_stride + first;
-    const int shift = (int)((reinterpret_cast<uintptr_t>(src) / sizeof(T)) % PIECE);
-    float top = -INFINITY;
-    auto one = [&](int place) {   // a place outside the part holds no logit; no number is none either
-        const int i = place - shift;
-        float x = i >= 0 && i < n ? load_as_float(src + i) : -INFINITY;
-        x = fmaxf(x, -INFINITY);
-        top = fmaxf(top, x);
-        if constexpr (sizeof(T) == 4) x_s[place] = x;
-        else x_s[place] = __float2bfloat16_rn(x);
-    };
-    {
-        // pieces that lie wholly inside: [1 or 0, whole)
-        const int begin = shift ? 1 : 0, whole = (shift + n) / PIECE;
-        const uint4 *from = reinterpret_cast<const uint4 *>(src - shift);
-        uint4 *to = reinterpret_cast<uint4 *>(x_s);
-#pragma unroll 8
-        for (int i = begin + tid; i < whole; i += SA_THREADS) {
-            uint4 u = __ldg(from + i);
-            if constexpr (sizeof(T) == 4) {
+    const int shift = (int)((reinterpret_cast<uintptr_t>(src) / sizeof(T)) % PIECE), end = shift + n;
+    // a warp goes over its share of the places, four neighbouring ones per lane
+    const int from_place = warp * (places / SA_WARPS), to_place = min(from_place + places / SA_WARPS, (end + 3) / 4 * 4);
+    auto index_at = [&](int place) { return first + place - shift; };
+    const int in0 = (shift + 3) / 4 * 4, in1 = end / 4 * 4 - 4;   // the first and the last four places that lie wholly inside, if any do
+    auto from_row = [&](int i) {   // four logits where they come from; a place outside the part holds none
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        const int inside = min(max(i, in0), in1);   // (a load that waits for no comparison)
+        if (in0 <= in1) v = Quad<T>::get(src - shift + inside);
+        if (inside != i || in0 > in1) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float x = fmaxf(__uint_as_float((&u.x)[k]), -INFINITY);
-                    top = fmaxf(top, x);
-                    (&u.x)[k] = __float_as_uint(x);
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float a = fmaxf(__uint_as_float((&u.x)[k] << 16), -INFINITY), b = fmaxf(__uint_as_float((&u.x)[k] & 0xFFFF0000u), -INFINITY);
-                    top = fmaxf(top, fmaxf(a, b));
-                    (&u.x)[k] = __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xFFFF0000u);
-                }
-            }
-            to[i] = u;
+            for (int j = 0; j < 4; ++j) (&v.x)[j] = i + j >= shift && i + j < end ? load_as_float(src - shift + i + j) : -INFINITY;
         }
-        const int behind = max(whole, begin) * PIECE;
-        if (tid < begin * PIECE) one(tid);
-        for (int i = behind + tid; i < places; i += SA_THREADS) one(i);
+        return v;
+    };
+    bool infinite = false;   // the largest logit is +inf: those that are count as 0, all others as none
+    auto quad = [&](int i) {
+        float4 v;
+        if constexpr (HELD) v = Quad<T>::get(x_s + i);
+        else v = from_row(i);
+        return v;
+    };
+    auto finite = [&](float4 &v) {
+        if (infinite) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (&v.x)[j] = (&v.x)[j] == INFINITY ? 0.f : -INFINITY;
+        }
+    };
+    // f(four logits, place) for all places of this lane, the next four on their way meanwhile
+    auto each = [&](auto f) {
+        int i = from_place + lane * 4;
+        float4 next = i < to_place ? quad(i) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (; i < to_place; i += 128) {
+            float4 v = next;
+            if (i + 128 < to_place) next = quad(i + 128);
+            finite(v);
+            f(v, i);
+        }
+    };
+    float top = -INFINITY;
+#pragma unroll 8
+    for (int i = from_place + lane * 4; i < to_place; i += 128) {
+        const float4 v = from_row(i);
+        top = fmaxf(fmaxf(fmaxf(top, v.x), v.y), fmaxf(v.z, v.w));   // (of a number and none, the number)
+        if constexpr (HELD) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(x_s + i) = v;
+            else *reinterpret_cast<uint2 *>(x_s + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+        }
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -254,22 +246,21 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
     cluster.sync();
     float m = -INFINITY;
     for (int r = 0; r < ranks; ++r) m = fmaxf(m, *cluster.map_shared_rank(&sh.top[SA_WARPS], r));
+    const bool here = sh.top[SA_WARPS] == m;   // this CTA has it
+    infinite = m == INFINITY;
+    if (infinite) m = 0.f;
 
     const float T_row = p.temperature ? p.temperature[row] : 1.f;
     const bool greedy = !(T_row > 0.f);
-    // a warp goes over its share of the places, four neighbouring ones per lane
-    const int from_place = warp * (places / SA_WARPS), to_place = from_place + places / SA_WARPS;
-    auto index_at = [&](int place) { return first + place - shift; };
 
     if (m == -INFINITY || greedy) {   // nothing to choose from, or the first of the largest
         int best = 0x7fffffff;
-        if (m > -INFINITY && sh.top[SA_WARPS] == m)
-            for (int i = from_place + lane * 4; i < to_place; i += 128) {
-                const float4 v = Quad<T>::get(x_s + i);
+        if (m > -INFINITY && here)
+            each([&](const float4 &v, int i) {
 #pragma unroll
                 for (int j = 3; j >= 0; --j)
                     if ((&v.x)[j] == m) best = min(best, index_at(i + j));
-            }
+            });
 #pragma unroll
         for (int off = 16; off; off >>= 1) best = min(best, __shfl_xor_sync(0xffffffffu, best, off));
         if (lane == 0) sh.best[warp] = best;
@@ -293,11 +284,13 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
     const bool by_k = k > 0, by_p = top_p < 1.f;
     const double per = fmin(1.4426950408889634 / (double)T_row, 1e30);
-    const float per_hi = (float)per, per_lo = (float)(per - (double)per_hi);
-    // (differences where per rounds to 0 are unbounded; a little inside SA_COARSE and SA_LAST whatever the quotients' rounding)
-    const Weigh weigh{m, per_hi, per_lo, fminf(SA_COARSE * 1.000001f / per_hi, 3e38f), fminf(SA_LAST / per_hi, 3e38f), m < INFINITY, sh.table, sh.table_4};
+    const float per_hi = (float)per, per_lo = (float)(per - (double)per_hi), d_last = SA_LAST / per_hi;
+    // coarse weights are of logits that are below 2^-6 whatever the roundings here; where logits lie so far apart that x_last cannot be
+    // told from m, or weights fall so slowly that differences overflow, all are weighed finely
+    const Weigh weigh{m, per_hi, per_lo, m - SA_COARSE * 1.001f / per_hi - fabsf(m) * 2.4e-7f, m - d_last,
+                      !(fabsf(m) * 2.4e-7f < 0.1f * d_last && fabsf(m) + d_last < 1e37f), sh.table, sh.table_4};
     const float to_bin = (float)fmin((double)SA_PER_NAT / (double)T_row, 1e30);
-    auto place_of = [&](float x) { return fmaxf(m - x, 0.f) * to_bin; };   // its whole part is the bin
+    auto place_of = [&](float x) { return (m - x) * to_bin; };   // its whole part is the bin; it falls as x rises (no number: in no bin)
 
     int turn = 0;
     // sums of three numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
@@ -339,14 +332,13 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
     u64 w = 0;              // this thread's share of the kept weights
     bool summed = false;    // where it is known already
     if (by_k || by_p) {
-        for (int i = from_place + lane * 4; i < to_place; i += 128) {
-            const float4 v = Quad<T>::get(x_s + i);
+        each([&](const float4 &v, int) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float b = place_of((&v.x)[j]);
                 if (b < (float)SA_BINS) atomicAdd(&sh.count[(int)b], 1u);
             }
-        }
+        });
         cluster.sync();
         // bins' counts over the cluster: each rank those of its share, then everybody reads all of them
         const int share = SA_BINS / ranks;
@@ -356,11 +348,11 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
             sh.count[i] = c;   // (of this bin no other rank reads this copy)
         }
         cluster.sync();
-        uint32_t c2[2], cb;    // this thread's two bins, and the counts of all in front of them
+        uint32_t own[SA_OWN], mine = 0, cb;   // this thread's bins, their sum, and the counts of all in front of them
 #pragma unroll
-        for (int j = 0; j < 2; ++j) c2[j] = *cluster.map_shared_rank(&sh.count[2 * tid + j], (2 * tid + j) / share);
+        for (int j = 0; j < SA_OWN; ++j) mine += own[j] = *cluster.map_shared_rank(&sh.count[SA_OWN * tid + j], (SA_OWN * tid + j) / share);
         {
-            uint32_t c = c2[0] + c2[1];
+            uint32_t c = mine;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
                 const uint32_t up = __shfl_up_sync(0xffffffffu, c, off);
@@ -369,7 +361,7 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
             if (lane == 31) sh.scan_n[warp] = c;
             if (tid == 0) sh.bin = SA_BINS;
             __syncthreads();
-            cb = c - c2[0] - c2[1];
+            cb = c - mine;
             for (int i = 0; i < warp; ++i) cb += sh.scan_n[i];
         }
         auto in_bin = [&](float b, int bin) { return b >= (float)bin && b < (float)(bin + 1); };
@@ -432,8 +424,7 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
                 while (lo < hi) {
                     const u64 mid = lo + (hi - lo) / 2;
                     u64 a[3] = {0, 0, 0}, all[3];
-                    for (int i = from_place + lane * 4; i < to_place; i += 128) {
-                        const float4 v = Quad<T>::get(x_s + i);
+                    each([&](const float4 &v, int i) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float x = (&v.x)[j], b = place_of(x);
@@ -442,7 +433,7 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
                                 if (weights) a[0] += weigh.fine(x);
                             }
                         }
-                    }
+                    });
                     cluster_sum(a, all, nullptr);
                     if (all[1] && enough((uint32_t)all[1], all[0])) hi = mid;
                     else lo = mid + 1;
@@ -460,22 +451,21 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
         if (by_k) {   // the bin in which the k-th token lies, and its key
             uint32_t c = cb;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (c < (uint32_t)k && (uint32_t)k <= c + c2[j]) {
-                    sh.bin = 2 * tid + j;
+            for (int j = 0; j < SA_OWN; ++j) {
+                if (c < (uint32_t)k && (uint32_t)k <= c + own[j]) {
+                    sh.bin = SA_OWN * tid + j;
                     sh.before_n = c;
                 }
-                c += c2[j];
+                c += own[j];
             }
             __syncthreads();
             const int bin = sh.bin;
             if (bin < SA_BINS) {   // (else all that weigh anything are among the first k)
                 const uint32_t wanted = (uint32_t)k - sh.before_n;
-                for (int i = from_place + lane * 4; i < to_place; i += 128) {
-                    const float4 v = Quad<T>::get(x_s + i);
+                each([&](const float4 &v, int i) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) gather(place_of((&v.x)[j]), (&v.x)[j], i + j, bin);
-                }
+                });
                 cluster.sync();
                 const u64 key = end_in_list(bin, false, [&](uint32_t cc, u64) { return cc >= wanted; });
                 empty_list();
@@ -485,17 +475,17 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
         }
         if (by_p) {
             // weights by the counts, in units; of the prefix so far, whose last bin counts as far as it belongs to it
-            float a2[2], ab;
+            float about[SA_OWN], ab, a_mine = 0.f;
             {
                 uint32_t c = cb;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int bin = 2 * tid + j;
-                    const float in = bin < cut_bin ? (float)c2[j] : bin == cut_bin ? (float)((uint32_t)k - c) : 0.f;
-                    a2[j] = in * exp2f((float)SA_UNIT - ((float)bin + 0.5f) * (1.4426950408889634f / SA_PER_NAT));
-                    c += c2[j];
+                for (int j = 0; j < SA_OWN; ++j) {
+                    const int bin = SA_OWN * tid + j;
+                    const float in = bin < cut_bin ? (float)own[j] : bin == cut_bin ? (float)((uint32_t)k - c) : 0.f;
+                    a_mine += about[j] = in * exp2f((float)SA_UNIT - ((float)bin + 0.5f) * (1.4426950408889634f / SA_PER_NAT));
+                    c += own[j];
                 }
-                float a = a2[0] + a2[1];
+                float a = a_mine;
 #pragma unroll
                 for (int off = 1; off < 32; off <<= 1) {
                     const float up = __shfl_up_sync(0xffffffffu, a, off);
@@ -503,7 +493,8 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
                 }
                 if (lane == 31) sh.scan_a[warp] = a;
                 __syncthreads();
-                ab = a - a2[0] - a2[1];
+                ab = __shfl_up_sync(0xffffffffu, a, 1);
+                if (lane == 0) ab = 0.f;
                 for (int i = 0; i < warp; ++i) ab += sh.scan_a[i];
             }
             float estimate = 0.f;   // of everything
@@ -518,10 +509,10 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
                 __syncthreads();
                 float a = ab;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int bin = 2 * tid + j;
-                    a += a2[j];
-                    if (bin > from && bin < to && c2[j] && bin <= cut_bin) {
+                for (int j = 0; j < SA_OWN; ++j) {
+                    const int bin = SA_OWN * tid + j;
+                    a += about[j];
+                    if (bin > from && bin < to && own[j] && bin <= cut_bin) {
                         if (a >= goal) atomicMin(&sh.bin, bin);
                         atomicMax(&sh.best[0], bin);
                     }
@@ -534,31 +525,25 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
             u64 up = 0, z = 0;
             while (bin >= 0) {   // ends: the bins between low and high get fewer
                 u64 a[3] = {0, 0, 0}, all[3], keep = 0;   // up to the bin, inside it, all of the prefix
-                for (int i = from_place + lane * 4; i < to_place; i += 128) {
-                    const float4 v = Quad<T>::get(x_s + i);
+                const float to = (float)bin, behind = (float)(bin + 1);
+                each([&](const float4 &v, int i) {
                     u64 w4[4];
-                    float b[4];
-                    bool any = false;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        b[j] = place_of((&v.x)[j]);
-                        any |= b[j] < (float)(cut_bin + 1);
-                    }
-                    if (!any) continue;
                     weigh.four(v, w4);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        if (by_k && !inside(b[j], (&v.x)[j], i + j)) continue;
+                        const float x = (&v.x)[j], b = place_of(x);
+                        if (by_k && !inside(b, x, i + j)) continue;
                         a[2] += w4[j];
-                        if (b[j] < (float)bin) {
+                        if (b < to) {
                             a[0] += w4[j];
-                            if (w4[j] >= least) keep += w4[j];
-                        } else if (b[j] < (float)(bin + 1)) {
+                            if (least && w4[j] >= least) keep += w4[j];
+                        } else if (b < behind) {
                             a[1] += w4[j];
-                            gather(b[j], (&v.x)[j], i + j, bin);
+                            gather(b, x, i + j, bin);
                         }
                     }
-                }
+                });
+                if (!least) keep = a[0];
                 cluster_sum(a, all, nullptr);
                 up = all[0];
                 z = all[2];
@@ -572,11 +557,16 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
                 }
                 empty_list();
                 // the estimate again, from the sums that are now known: the threads' prefix sums are compared with a goal that is moved
-                float at_bin = ab;
-                if (tid == bin / 2) {
-                    if (bin & 1) at_bin += a2[0];
-                    sh.scan_a[0] = at_bin;                                             // estimated up to the bin
-                    sh.scan_a[1] = bin & 1 ? a2[1] : a2[0];
+                if (tid == bin / SA_OWN) {
+                    float a = ab;
+#pragma unroll
+                    for (int j = 0; j < SA_OWN; ++j) {
+                        if (j == bin % SA_OWN) {
+                            sh.scan_a[0] = a;                                          // estimated up to the bin
+                            sh.scan_a[1] = about[j];
+                        }
+                        a += about[j];
+                    }
                 }
                 __syncthreads();
                 const float moved = high == bin ? (float)(goal - (double)up) + sh.scan_a[0]
@@ -607,33 +597,40 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
     }
 
     // ---- the kept weights: of each warp, of the warps in front, of all
+    const bool some = cut_bin < SA_BINS;   // not all are kept
+    const float cut_from = (float)cut_bin, cut_behind = some ? (float)(cut_bin + 1) : INFINITY;
     auto kept_four = [&](const float4 &v, int place, u64 (&own)[4]) {
-        float b[4];
-        bool any = false;
+        if (some) {   // (as a rule few are kept)
+            const float x = fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w));
+            if (!(place_of(x) < cut_behind)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            own[j] = 0;
-            b[j] = place_of((&v.x)[j]);
-            any |= b[j] < (float)(cut_bin + 1);
+                for (int j = 0; j < 4; ++j) own[j] = 0;
+                return;
+            }
         }
-        if (!any) return;
-        u64 w4[4];
-        weigh.four(v, w4);
+        weigh.four(v, own);
+        if (some) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (cut_bin < SA_BINS && !inside(b[j], (&v.x)[j], place + j)) continue;
-            // (members of the last bin are weighed as the list's are)
-            const u64 ww = cut_bin < SA_BINS && b[j] >= (float)cut_bin ? weigh.fine((&v.x)[j]) : w4[j];
-            own[j] = ww >= least ? ww : 0;
+            for (int j = 0; j < 4; ++j) {
+                const float b = place_of((&v.x)[j]);
+                if (b < cut_from) continue;
+                // (members of the last bin are weighed as the list's are)
+                own[j] = b < cut_behind && key_of((&v.x)[j], index_at(place + j)) <= cut_key ? weigh.fine((&v.x)[j]) : 0;
+            }
+        }
+        if (least) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (own[j] < least) own[j] = 0;
         }
     };
     if (!summed)
-        for (int i = from_place + lane * 4; i < to_place; i += 128) {
+        each([&](const float4 &v, int i) {
             u64 own[4];
-            kept_four(Quad<T>::get(x_s + i), i, own);
+            kept_four(v, i, own);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w += own[j];
-        }
+        });
     u64 sums[3] = {w, 0, 0}, all[3], before;
     cluster_sum(sums, all, &before);
     const u64 z = all[0];
@@ -648,7 +645,8 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
             u64 own[4] = {0, 0, 0, 0};
             float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
             if (i + lane * 4 < to_place) {
-                v = Quad<T>::get(x_s + i + lane * 4);
+                v = quad(i + lane * 4);
+                finite(v);
                 kept_four(v, i + lane * 4, own);
             }
             const u64 four = own[0] + own[1] + own[2] + own[3];
@@ -681,16 +679,20 @@ template <typename T> __global__ void __launch_bounds__(SA_THREADS, 2) sample_ke
 
 cudaError_t launch_sample(const SampleParams &p, bool bf16, cudaStream_t stream)
 {
-    // CTAs of a row: as many as keep the SMs busy, up to eight, none with less than 4096 logits
+    // CTAs of a row: as many as are resident at once for all rows together (up to 592), one to eight, none with less than 2048 logits.
     int ranks = 1;
-    while (ranks < 8 && p.vocab > 4096 * ranks && (p.n_rows * ranks < 2 * 148 || p.vocab > 16384 * ranks)) ranks *= 2;
+    while (ranks < 8 && p.vocab > 2048 * ranks && (long long)p.n_rows * ranks * 2 <= SA_CTAS * AT_SMS) ranks *= 2;
     const int chunk = ((p.vocab + ranks - 1) / ranks + 7) / 8 * 8;
-    const int step = 8 * SA_WARPS, places = (chunk + 8 + step - 1) / step * step;   // (up to seven in front of a row's part: 16-byte pieces)
-    const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (size_t)places * (bf16 ? 2 : 4);
-    static PerContext seen[2];
-    const auto kernel = bf16 ? sample_kernel<__nv_bfloat16> : sample_kernel<float>;
+    const int step = 8 * SA_WARPS, places = (chunk + 8 + step - 1) / step * step;   // (up to seven in front of a row's part: 16-byte boundaries)
+    const bool held = (size_t)places * (bf16 ? 2 : 4) <= SA_HELD;
+    const size_t smem = (sizeof(SampleShared) + 15) / 16 * 16 + (held ? (size_t)places * (bf16 ? 2 : 4) : 0);
+    static PerContext seen[4];
+    using Kernel = void (*)(const SampleParams, int, int);
+    static const Kernel kernels[4] = {sample_kernel<float, false>, sample_kernel<float, true>, sample_kernel<__nv_bfloat16, false>,
+                                      sample_kernel<__nv_bfloat16, true>};
+    const int which = (bf16 ? 2 : 0) + (held ? 1 : 0);
     int sms = 0;
-    const cudaError_t e = device_sms(seen[bf16], reinterpret_cast<const void *>(kernel), 220 << 10, &sms);
+    const cudaError_t e = device_sms(seen[which], reinterpret_cast<const void *>(kernels[which]), (sizeof(SampleShared) + 15) / 16 * 16 + SA_HELD, &sms);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.n_rows * ranks));
@@ -706,7 +708,7 @@ cudaError_t launch_sample(const SampleParams &p, bool bf16, cudaStream_t stream)
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, p, chunk, places);
+    return cudaLaunchKernelEx(&cfg, kernels[which], p, chunk, places);
 }
 
 }  // namespace gdn
