@@ -14,6 +14,7 @@
 // altogether, and sees whether it is the one (else the estimate starts again from these sums).  Only that bin's members (some hundreds
 // of 131071) are put in order; a bin with more members than fit (many equal logits) is bisected instead.  What the pass summed up
 // to the bin, warp by warp, also says where the token lies.
+// The first k of a row, k up to a thousand, are put in order at once, and the row is done with.
 //
 // A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-38 (no order
 // of additions matters).  Those of 2^-6 and more are formed to about 1e-9 of themselves, the others to fp32: their errors are as often
@@ -65,6 +66,7 @@ struct SampleShared {
     float scan_a[SA_WARPS];
     int bin;
     uint32_t before_n;
+    bool few;                           // tokens down to the end of `bin`
 };
 
 // Weights in units of tokens with given logits; per = log2(e) / T in two parts.
@@ -188,50 +190,74 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     // a warp goes over its share of the places, four neighbouring ones per lane
     const int from_place = warp * (places / SA_WARPS), to_place = min(from_place + places / SA_WARPS, (end + 3) / 4 * 4);
     auto index_at = [&](int place) { return first + place - shift; };
-    const int in0 = (shift + 3) / 4 * 4, in1 = end / 4 * 4 - 4;   // the first and the last four places that lie wholly inside, if any do
-    auto from_row = [&](int i) {   // four logits where they come from; a place outside the part holds none
-        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        const int inside = min(max(i, in0), in1);   // (a load that waits for no comparison)
-        if (in0 <= in1) v = Quad<T>::get(src - shift + inside);
-        if (inside != i || in0 > in1) {
+    const int in0 = (shift + 3) / 4 * 4, in1 = end / 4 * 4;   // [in0, in1): fours of places that lie wholly inside
+    auto from_row = [&](int i, int warp_at) {   // four logits where they come from; the warp is at places warp_at ... + 127
+        if (warp_at >= in0 && warp_at + 128 <= in1) return Quad<T>::get(src - shift + i);
+        float4 v;   // a place outside the part holds none
 #pragma unroll
-            for (int j = 0; j < 4; ++j) (&v.x)[j] = i + j >= shift && i + j < end ? load_as_float(src - shift + i + j) : -INFINITY;
-        }
+        for (int j = 0; j < 4; ++j) (&v.x)[j] = i + j >= shift && i + j < end ? load_as_float(src - shift + i + j) : -INFINITY;
         return v;
     };
     bool infinite = false;   // the largest logit is +inf: those that are count as 0, all others as none
-    auto quad = [&](int i) {
-        float4 v;
-        if constexpr (HELD) v = Quad<T>::get(x_s + i);
-        else v = from_row(i);
-        return v;
+    auto quad = [&](int i, int warp_at) {
+        if constexpr (HELD) return Quad<T>::get(x_s + i);
+        else return from_row(i, warp_at);
     };
-    auto finite = [&](float4 &v) {
+    auto as_finite = [&](float4 &v) {
         if (infinite) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) (&v.x)[j] = (&v.x)[j] == INFINITY ? 0.f : -INFINITY;
         }
     };
-    // f(four logits, place) for all places of this lane, the next four on their way meanwhile
-    auto each = [&](auto f) {
-        int i = from_place + lane * 4;
-        float4 next = i < to_place ? quad(i) : make_float4(0.f, 0.f, 0.f, 0.f);
-        for (; i < to_place; i += 128) {
+    // f(four logits, place) for this lane's fours of places [from, to) (of the whole warp), the next ones on their way meanwhile
+    auto each = [&](int from, int to, auto f) {
+        if (from >= to) return;
+        const int mine = lane * 4;
+        float4 next = from + mine < to ? quad(from + mine, from) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        for (int at = from; at < to; at += 128) {
             float4 v = next;
-            if (i + 128 < to_place) next = quad(i + 128);
-            finite(v);
-            f(v, i);
+            if (at + 128 + mine < to) next = quad(at + 128 + mine, at + 128);
+            as_finite(v);
+            if (at + mine < to) f(v, at + mine);
+        }
+    };
+    // the same for an f too short to wait behind: eight loads on their way
+    auto each_short = [&](int from, int to, auto f) {
+        constexpr int N = HELD ? 1 : 8;
+        for (int at = from; at < to; at += N * 128) {
+            float4 v[N];
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (at + k * 128 + lane * 4 < to) v[k] = quad(at + k * 128 + lane * 4, at + k * 128);
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                as_finite(v[k]);
+                if (at + k * 128 + lane * 4 < to) f(v[k], at + k * 128 + lane * 4);
+            }
         }
     };
     float top = -INFINITY;
-#pragma unroll 8
-    for (int i = from_place + lane * 4; i < to_place; i += 128) {
-        const float4 v = from_row(i);
+    auto take = [&](const float4 &v, int i) {
         top = fmaxf(fmaxf(fmaxf(top, v.x), v.y), fmaxf(v.z, v.w));   // (of a number and none, the number)
         if constexpr (HELD) {
             if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(x_s + i) = v;
             else *reinterpret_cast<uint2 *>(x_s + i) = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
         }
+    };
+    {
+        int at = from_place;
+        for (; at < to_place && at < in0; at += 128)
+            if (at + lane * 4 < to_place) take(from_row(at + lane * 4, at), at + lane * 4);
+        for (; at + 8 * 128 <= min(to_place, in1); at += 8 * 128) {   // eight loads on their way
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = Quad<T>::get(src - shift + at + k * 128 + lane * 4);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) take(v[k], at + k * 128 + lane * 4);
+        }
+#pragma unroll 4
+        for (; at < to_place; at += 128)
+            if (at + lane * 4 < to_place) take(from_row(at + lane * 4, at), at + lane * 4);
     }
 #pragma unroll
     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -256,7 +282,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     if (m == -INFINITY || greedy) {   // nothing to choose from, or the first of the largest
         int best = 0x7fffffff;
         if (m > -INFINITY && here)
-            each([&](const float4 &v, int i) {
+            each_short(from_place, to_place, [&](const float4 &v, int i) {
 #pragma unroll
                 for (int j = 3; j >= 0; --j)
                     if ((&v.x)[j] == m) best = min(best, index_at(i + j));
@@ -332,7 +358,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     u64 w = 0;              // this thread's share of the kept weights
     bool summed = false;    // where it is known already
     if (by_k || by_p) {
-        each([&](const float4 &v, int) {
+        each_short(from_place, to_place, [&](const float4 &v, int) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float b = place_of((&v.x)[j]);
@@ -372,29 +398,33 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                 if (at < SA_SORT) cluster.map_shared_rank(sh.sorted, 0)[at] = key_of(x, index_at(place));
             }
         };
+        // by rank 0: the list in order, by exchanges at distances that are powers of two; where `have` are fewer than such a power, `none` behind
+        auto sort_list = [&](int have) {
+            int size = 32;
+            while (size < have) size *= 2;
+            for (int i = have + tid; i < size; i += SA_THREADS) sh.sorted[i] = ~0ull;
+            __syncthreads();
+            for (int run = 2; run <= size; run *= 2)
+                for (int apart = run / 2; apart; apart /= 2) {
+                    for (int i = tid; i < size / 2; i += SA_THREADS) {
+                        const int a = 2 * i - (i & (apart - 1)), b = a + apart;
+                        const u64 ka = sh.sorted[a], kb = sh.sorted[b];
+                        if ((ka > kb) == ((a & run) == 0)) {
+                            sh.sorted[a] = kb;
+                            sh.sorted[b] = ka;
+                        }
+                    }
+                    __syncthreads();
+                }
+        };
         // The smallest key of the bin's members in the list up to which `enough` holds of the (count, weight) of those with keys up to it;
         // where they were too many for the list, found bit by bit, each with a pass over the row.  After a barrier of the cluster.
         auto end_in_list = [&](int bin, bool weights, auto enough) {
             const int have = *cluster.map_shared_rank(&sh.members, 0);
             u64 key = ~0ull;
             if (have <= SA_SORT) {
-                if (rank == 0) {   // in order by exchanges at distances that are powers of two
-                    int size = 32;
-                    while (size < have) size *= 2;
-                    for (int i = have + tid; i < size; i += SA_THREADS) sh.sorted[i] = ~0ull;
-                    __syncthreads();
-                    for (int run = 2; run <= size; run *= 2)
-                        for (int apart = run / 2; apart; apart /= 2) {
-                            for (int i = tid; i < size / 2; i += SA_THREADS) {
-                                const int a = 2 * i - (i & (apart - 1)), b = a + apart;
-                                const u64 ka = sh.sorted[a], kb = sh.sorted[b];
-                                if ((ka > kb) == ((a & run) == 0)) {
-                                    sh.sorted[a] = kb;
-                                    sh.sorted[b] = ka;
-                                }
-                            }
-                            __syncthreads();
-                        }
+                if (rank == 0) {
+                    sort_list(have);
                     // the first member up to which it is enough, by one warp, 32 members at a time
                     if (warp == 0) {
                         u64 sum = 0;
@@ -424,7 +454,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                 while (lo < hi) {
                     const u64 mid = lo + (hi - lo) / 2;
                     u64 a[3] = {0, 0, 0}, all[3];
-                    each([&](const float4 &v, int i) {
+                    each(from_place, to_place, [&](const float4 &v, int i) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const float x = (&v.x)[j], b = place_of(x);
@@ -455,14 +485,97 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                 if (c < (uint32_t)k && (uint32_t)k <= c + own[j]) {
                     sh.bin = SA_OWN * tid + j;
                     sh.before_n = c;
+                    sh.few = c + own[j] <= SA_SORT;
                 }
                 c += own[j];
             }
             __syncthreads();
             const int bin = sh.bin;
+            if (k <= SA_SORT && bin < SA_BINS && sh.few) {
+                // all tokens down to that bin fit the list: the rest goes on there, without the row
+                each_short(from_place, to_place, [&](const float4 &v, int i) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (place_of((&v.x)[j]) < (float)(bin + 1)) {
+                            const int at = atomicAdd(cluster.map_shared_rank(&sh.members, 0), 1);
+                            cluster.map_shared_rank(sh.sorted, 0)[at] = key_of((&v.x)[j], index_at(i + j));
+                        }
+                });
+                cluster.sync();
+                if (rank != 0) return;   // (nobody reads its shared memory any more)
+                sort_list(sh.members);
+                // weights' sums in falling order, by one warp; how many are kept of the first k
+                int kept_n = k;
+                if (warp == 0) {
+                    u64 total = 0;
+                    for (int pass = 0; pass < 2; ++pass) {   // the sum of the first k, then the prefix
+                        const double goal = (double)top_p * (double)total;
+                        u64 sum = 0;
+                        bool over = false;
+                        for (int i = 0; i < k && !over; i += 32) {
+                            const bool there = i + lane < k;
+                            u64 upto = there ? weigh.fine(logit_of(sh.sorted[i + lane])) : 0;
+                            const u64 own_w = upto;
+#pragma unroll
+                            for (int off = 1; off < 32; off <<= 1) {
+                                const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
+                                if (lane >= off) upto += up;
+                            }
+                            if (pass == 1) {
+                                const bool ends = there && ((by_p && (i + lane > 0) && (double)(sum + upto - own_w) >= goal) || own_w < least || own_w == 0);
+                                const unsigned yes = __ballot_sync(0xffffffffu, ends);
+                                if (yes) {
+                                    kept_n = i + __ffs(yes) - 1;
+                                    over = true;
+                                }
+                            }
+                            sum += __shfl_sync(0xffffffffu, upto, 31);
+                        }
+                        if (pass == 0) total = sum;
+                    }
+                    if (lane == 0) sh.members = kept_n;
+                }
+                __syncthreads();
+                kept_n = sh.members;
+                // by index: the place in the falling order stands in the lower half of a key meanwhile
+                for (int i = tid; i < kept_n; i += SA_THREADS) {
+                    const u64 key = sh.sorted[i];
+                    sh.sorted[i] = key << 32 | key >> 32;
+                }
+                __syncthreads();
+                sort_list(kept_n);
+                if (warp == 0) {
+                    auto logit_at = [&](int i) { return logit_of(sh.sorted[i] << 32); };
+                    u64 z = 0;
+                    for (int i = lane; i < kept_n; i += 32) z += weigh.fine(logit_at(i));
+#pragma unroll
+                    for (int off = 16; off; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
+                    double u = (double)p.uniform[row];
+                    u = u >= 0.0 ? u : 0.0;
+                    const double at = u * (double)z;
+                    const u64 goal = at < (double)z ? min((u64)at, z - 1) : z - 1;
+                    u64 sum = 0;
+                    for (int i = 0; i < kept_n; i += 32) {
+                        const float x = i + lane < kept_n ? logit_at(i + lane) : -INFINITY;
+                        const u64 own_w = i + lane < kept_n ? weigh.fine(x) : 0;
+                        u64 upto = own_w;
+#pragma unroll
+                        for (int off = 1; off < 32; off <<= 1) {
+                            const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
+                            if (lane >= off) upto += up;
+                        }
+                        if (sum + upto - own_w <= goal && goal < sum + upto) {
+                            p.token[row] = (int)(sh.sorted[i + lane] >> 32);
+                            if (p.prob) p.prob[row] = (float)(weigh.exactly(x) / (double)z);
+                        }
+                        sum += __shfl_sync(0xffffffffu, upto, 31);
+                    }
+                }
+                return;
+            }
             if (bin < SA_BINS) {   // (else all that weigh anything are among the first k)
                 const uint32_t wanted = (uint32_t)k - sh.before_n;
-                each([&](const float4 &v, int i) {
+                each_short(from_place, to_place, [&](const float4 &v, int i) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) gather(place_of((&v.x)[j]), (&v.x)[j], i + j, bin);
                 });
@@ -526,7 +639,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
             while (bin >= 0) {   // ends: the bins between low and high get fewer
                 u64 a[3] = {0, 0, 0}, all[3], keep = 0;   // up to the bin, inside it, all of the prefix
                 const float to = (float)bin, behind = (float)(bin + 1);
-                each([&](const float4 &v, int i) {
+                each(from_place, to_place, [&](const float4 &v, int i) {
                     u64 w4[4];
                     weigh.four(v, w4);
 #pragma unroll
@@ -625,7 +738,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
         }
     };
     if (!summed)
-        each([&](const float4 &v, int i) {
+        each(from_place, to_place, [&](const float4 &v, int i) {
             u64 own[4];
             kept_four(v, i, own);
 #pragma unroll
@@ -634,43 +747,66 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     u64 sums[3] = {w, 0, 0}, all[3], before;
     cluster_sum(sums, all, &before);
     const u64 z = all[0];
-    w = sums[0];   // of the warp
     double u = (double)p.uniform[row];
     u = u >= 0.0 ? u : 0.0;   // (no number: 0)
     const double at = u * (double)z;
     const u64 goal = at < (double)z ? min((u64)at, z - 1) : z - 1;
-    if (before <= goal && goal < before + w) {   // this warp alone
-        u64 sum = before;
-        for (int i = from_place; i < to_place; i += 128) {
-            u64 own[4] = {0, 0, 0, 0};
-            float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-            if (i + lane * 4 < to_place) {
-                v = quad(i + lane * 4);
-                finite(v);
-                kept_four(v, i + lane * 4, own);
-            }
-            const u64 four = own[0] + own[1] + own[2] + own[3];
-            u64 upto = four;
+    // whose share holds the token: a warp's, then, all warps of its CTA over that one, an eighth of it, which one warp goes through
+    const u64 *parts = sh.sum[turn ^ 1][0];   // the warps' sums
+    u64 at_warp = before;
+    for (int i = 0; i < warp; ++i) at_warp -= parts[i];
+    const bool in_cta = at_warp <= goal && goal < at_warp + parts[SA_WARPS];
+    if (in_cta) {
+        int chosen = 0;
+        while (goal >= at_warp + parts[chosen]) at_warp += parts[chosen++];
+        const int share = places / SA_WARPS, part = (share / 8 + SA_WARPS - 1) / SA_WARPS * 8;   // (of places: a multiple of 8)
+        const int lo = chosen * share, hi = min(lo + share, (end + 3) / 4 * 4);
+        const int from = min(lo + warp * part, hi), to = min(from + part, hi);
+        u64 mine = 0;
+        each(from, to, [&](const float4 &v, int i) {
+            u64 own[4];
+            kept_four(v, i, own);
+            mine += (own[0] + own[1]) + (own[2] + own[3]);
+        });
 #pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
-                if (lane >= off) upto += up;
-            }
-            const u64 quads = __shfl_sync(0xffffffffu, upto, 31);
-            if (goal < sum + quads) {
-                u64 s = sum + upto - four;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (s <= goal && goal < s + own[j]) {
-                        p.token[row] = index_at(i + lane * 4 + j);
-                        if (p.prob) p.prob[row] = (float)(weigh.exactly((&v.x)[j]) / (double)z);
-                    }
-                    s += own[j];
+        for (int off = 16; off; off >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, off);
+        u64 *eighths = sh.sum[turn][0];
+        if (lane == 0) eighths[warp] = mine;
+        __syncthreads();
+        u64 sum = at_warp;
+        for (int i = 0; i < warp; ++i) sum += eighths[i];
+        if (sum <= goal && goal < sum + mine)
+            for (int at = from; at < to; at += 128) {
+                const int i = at + lane * 4;
+                u64 own[4] = {0, 0, 0, 0};
+                float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                if (i < to) {
+                    v = quad(i, at);
+                    as_finite(v);
+                    kept_four(v, i, own);
                 }
-                break;
+                const u64 four = own[0] + own[1] + own[2] + own[3];
+                u64 upto = four;
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
+                    if (lane >= off) upto += up;
+                }
+                const u64 quads = __shfl_sync(0xffffffffu, upto, 31);
+                if (goal < sum + quads) {
+                    u64 s = sum + upto - four;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (s <= goal && goal < s + own[j]) {
+                            p.token[row] = index_at(i + j);
+                            if (p.prob) p.prob[row] = (float)(weigh.exactly((&v.x)[j]) / (double)z);
+                        }
+                        s += own[j];
+                    }
+                    break;
+                }
+                sum += quads;
             }
-            sum += quads;
-        }
     }
     cluster.sync();   // (nobody leaves while its shared memory is read)
 }
