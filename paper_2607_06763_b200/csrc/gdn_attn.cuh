@@ -97,6 +97,13 @@ __device__ __forceinline__ long long attn_seq_work(const AttnParams &p, int b, i
     return (long long)p.h_kv * ((s.rows * p.group + M - 1) / M) * attn_tiles(s, TN);
 }
 
+// a * b / c, by a 32-bit division wherever the product fits (a 64-bit one takes some hundred instructions).
+__device__ __forceinline__ long long times_over(long long a, long long b, long long c)
+{
+    const unsigned long long ab = (unsigned long long)a * (unsigned long long)b;
+    return ((ab | (unsigned long long)c) >> 32) == 0 ? (long long)((uint32_t)ab / (uint32_t)c) : (long long)(ab / (unsigned long long)c);
+}
+
 // Sum over the lanes up to and including this one.
 __device__ __forceinline__ long long warp_scan(long long x, int lane)
 {
@@ -133,8 +140,8 @@ struct AttnWalk {
         const long long runs = total < p.n_ctas ? total : p.n_ctas;
         at = end = 0;
         if (cta >= runs) return;
-        at = total * cta / runs;
-        end = total * (cta + 1) / runs;
+        at = times_over(total, cta, runs);
+        end = times_over(total, cta + 1, runs);
         // the lane whose sequences hold tile `at` looks for it among them
         const unsigned holds = __ballot_sync(0xffffffffu, upto > at);
         const int owner = __ffs(holds) - 1;
@@ -178,7 +185,7 @@ struct AttnWalk {
         g.s = s;
         g.b = b;
         g.tiles = attn_tiles(s, TN);
-        const int unit = (int)((at - seq_at) / g.tiles);
+        const int unit = (int)times_over(at - seq_at, 1, g.tiles);
         const int m_tiles = (s.rows * p.group + M - 1) / M;
         g.head = unit / m_tiles;
         g.m_tile = unit % m_tiles;
@@ -205,42 +212,44 @@ __device__ __forceinline__ long long attn_token_offset(const AttnParams &p, int 
     return page * p.page_stride + (t - entry * p.page_size) * p.token_stride;
 }
 
-// Ancestors of the nodes of a tree of at most 64 nodes, the node itself among them, by all threads of the CTA (at least 64);
-// a and up are [64] each.  False where the tree is none.  Doubling: after k rounds a node knows its next 2^k ancestors.
-__device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSeq &s, unsigned long long *a, int *up)
+// Ancestors of the nodes of a tree of at most 64 nodes, the node itself among them, for all threads of the CTA, by its first warp
+// (two nodes per lane); a and up are [64] each.  False where the tree is none.  Doubling: after k rounds a node knows its next 2^k
+// ancestors.
+__device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSeq &s, unsigned long long *a, int *up, int *good)
 {
-    const int i = threadIdx.x;
-    int parent = -1;
-    bool bad = false;
-    if (i < s.rows) {
-        parent = p.parent[s.row0 + i];
-        bad = parent < -1 || parent >= i;
-    }
-    if (__syncthreads_or(bad)) return false;
-    if (i < AT_SMALL_ROWS) {
-        a[i] = 1ull << i;
-        up[i] = parent;
+    const int lane = threadIdx.x;
+    if (lane < 32) {
+        int next[2];
+        unsigned long long seen[2];
+        bool bad = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane + 32 * h;
+            next[h] = i < s.rows ? p.parent[s.row0 + i] : -1;
+            bad |= next[h] < -1 || next[h] >= i;
+        }
+        bad = __any_sync(0xffffffffu, bad);
+        if (lane == 0) *good = !bad;
+        for (int step = 1; !bad && step < 2 * s.rows; step <<= 1) {   // (the last round only writes)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int i = lane + 32 * h;
+                if (step == 1) seen[h] = 1ull << i;
+                a[i] = seen[h];
+                up[i] = next[h];
+            }
+            __syncwarp();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (next[h] >= 0) {
+                    seen[h] |= a[next[h]];
+                    next[h] = up[next[h]];
+                }
+            __syncwarp();
+        }
     }
     __syncthreads();
-    for (int step = 1; step < s.rows; step <<= 1) {
-        unsigned long long mine = 0;
-        int next = -1;
-        if (i < AT_SMALL_ROWS) {
-            mine = a[i];
-            next = up[i];
-            if (next >= 0) {
-                mine |= a[next];
-                next = up[next];
-            }
-        }
-        __syncthreads();
-        if (i < AT_SMALL_ROWS) {
-            a[i] = mine;
-            up[i] = next;
-        }
-        __syncthreads();
-    }
-    return true;
+    return *good != 0;
 }
 
 // Whether row node i sees node j of its sequence's rows (i, j < rows).
@@ -262,7 +271,7 @@ constexpr int AT_SMS = 148;
 struct AttnTiling {
     int M, TN, ctas;   // rows and tokens of a tile, CTAs that an SM holds
 };
-AttnTiling attn_general_tiling();
+AttnTiling attn_general_tiling(bool bf16, int d);
 // `bf16`: the type of rows, cache and outputs; otherwise fp32.
 cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream);
 // bf16, d = 64 or 128, tiles of 16, 32 or 64 rows.

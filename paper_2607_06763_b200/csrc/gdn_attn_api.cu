@@ -46,7 +46,7 @@ bool choose(const gdn_attn_shape_t &s, Choice &c)
     // up to 64 rows per key/value head the keys and values decide, and one tile of rows reads them once; above, the products do.
     // (The kernel of the latter takes maxima of unscaled scores: a scale that turns or hides their order is the other's.)
     c.kernel = !(s.dtype == GDN_BF16 && (s.d == 64 || s.d == 128)) ? Choice::GENERAL : rows <= 64 || !(s.scale > 0.f) ? Choice::ROWS : Choice::SM100;
-    c.tiling = c.kernel == Choice::GENERAL ? attn_general_tiling() : c.kernel == Choice::ROWS ? attn_rows_tiling((int)rows, s.d) : attn_sm100_tiling();
+    c.tiling = c.kernel == Choice::GENERAL ? attn_general_tiling(s.dtype == GDN_BF16, s.d) : c.kernel == Choice::ROWS ? attn_rows_tiling((int)rows, s.d) : attn_sm100_tiling();
     c.m_tiles = (int)((rows + c.tiling.M - 1) / c.tiling.M);
     const long long units = (long long)s.n_seq * s.h_kv * c.m_tiles, tiles = ((long long)s.max_len + c.tiling.TN - 1) / c.tiling.TN;
     if (units > 0x7fffffffLL) return false;

@@ -19,7 +19,7 @@ constexpr int AG_STAGES = 2;
 template <typename T> __host__ __device__ constexpr int ag_pitch(int d) { return d * (int)sizeof(T) + 16; }   // the next row begins four banks on
 template <typename T> constexpr size_t ag_smem(int d)
 {
-    return (size_t)AG_STAGES * 2 * AG_TN * ag_pitch<T>(d) + AG_M * d * sizeof(float) + AG_M * AG_TN * sizeof(float);
+    return (size_t)AG_STAGES * 2 * AG_TN * ag_pitch<T>(d) + AG_M * d * sizeof(float) + 2 * AG_M * AG_TN * sizeof(float);
 }
 
 __device__ __forceinline__ float4 four(const float *p) { return *reinterpret_cast<const float4 *>(p); }
@@ -30,16 +30,19 @@ __device__ __forceinline__ float4 four(const __nv_bfloat16 *p)
                        __uint_as_float(u.y & 0xFFFF0000u));
 }
 
-// Four warps, each with four rows; a lane has a token in the products with the keys and four components in those with the
-// values.  Bound by shared memory for many rows (a key's four components feed sixteen multiplications), by HBM for few.
+// Four warps, each with four rows, or two or four of them with the same four where there are not enough: then each has a share of the
+// components in the products with the keys and of the tokens in those with the values.  A lane has a token in the former and four
+// components in the latter.  Bound by shared memory for many rows (a key's four components feed sixteen multiplications), by HBM for few.
 template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general_kernel(const AttnParams p)
 {
     extern __shared__ __align__(16) unsigned char ag_smem_base[];
     __shared__ unsigned long long anc[AT_SMALL_ROWS];
-    __shared__ int anc_up[AT_SMALL_ROWS];
+    __shared__ int anc_up[AT_SMALL_ROWS], tree_good;
     const int d = p.d, pitch = ag_pitch<T>(d), stage_bytes = 2 * AG_TN * pitch;
     float *q_s = reinterpret_cast<float *>(ag_smem_base + AG_STAGES * stage_bytes);
-    float *w_s = q_s + AG_M * d;
+    float *x_s = reinterpret_cast<float *>(ag_smem_base);   // at the end, over the tiles: [4 warps][4 rows][d], sums of warps that share rows
+    float *w_s = q_s + AG_M * d;        // [4 warps][AG_TN][4]: weights
+    float *s_s = w_s + AG_M * AG_TN;    // [4 warps][4][AG_TN]: scores over a warp's share of the components
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = (int)blockIdx.x;
     const AttnMaskKind kind = attn_mask_kind(p);
     const T *k_cache = static_cast<const T *>(p.k_cache), *v_cache = static_cast<const T *>(p.v_cache);
@@ -49,7 +52,7 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
     AttnSegment g;
     walk.begin(p, cta, AG_M, AG_TN);
     while (walk.next(p, cta, AG_M, AG_TN, g)) {
-        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up)) {
+        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up, &tree_good)) {
             if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
             continue;
         }
@@ -60,6 +63,7 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
             q_s[i] = load_as_float(static_cast<const T *>(p.q) + (size_t)(g.s.row0 + node) * p.q_stride +
                                    (size_t)(g.head * p.group + r % p.group) * d + i % d);
         }
+        const int with = rows <= 4 ? 4 : rows <= 8 ? 2 : 1, part = warp % with, row_group = warp / with;   // warps with the same rows
         // the last token that any of these rows sees: rows come in an order in which ancestors are in front
         const int last_node = (row_first + rows - 1) / p.group, upto = p.row_offsets ? g.s.len + last_node + 1 : g.s.len;
         const int tile1 = min(g.tile1, max((upto + AG_TN - 1) / AG_TN, g.tile0));
@@ -94,12 +98,13 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
             fetch(tile + 1);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
-            if (warp * 4 < rows) {
+            const bool busy = row_group * 4 < rows;
+            float sc[4] = {0.f, 0.f, 0.f, 0.f};
+            if (busy) {
                 const T *k_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + lane * pitch);
-                float sc[4] = {0.f, 0.f, 0.f, 0.f};
-                const float *qw = q_s + warp * 4 * d;
+                const float *qw = q_s + row_group * 4 * d;
 #pragma unroll 4
-                for (int c = 0; c < d; c += 4) {
+                for (int c = part * 4; c < d; c += with * 4) {
                     const float4 k4 = four(k_s + c);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
@@ -107,11 +112,25 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
                         sc[r] = fmaf(q4.x, k4.x, fmaf(q4.y, k4.y, fmaf(q4.z, k4.z, fmaf(q4.w, k4.w, sc[r]))));
                     }
                 }
+                if (with > 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s_s[(warp * 4 + r) * AG_TN + lane] = sc[r];
+                }
+            }
+            if (with > 1) __syncthreads();
+            if (busy) {
+                if (with > 1) {
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        sc[r] = 0.f;
+                        for (int o = 0; o < with; ++o) sc[r] += s_s[((row_group * with + o) * 4 + r) * AG_TN + lane];
+                    }
+                }
                 const int t = tile * AG_TN + lane;
                 float4 w;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = warp * 4 + r, node = (row_first + row) / p.group;
+                    const int row = row_group * 4 + r, node = (row_first + row) / p.group;
                     const bool seen = row < rows && (t < g.s.len || (t < g.s.held && attn_sees(p, kind, anc, g.s.row0, node, t - g.s.len)));
                     const float x = seen ? sc[r] * p.scale_log2 : -INFINITY;
                     float top = x;
@@ -134,7 +153,7 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
                 if (lane * 4 < d) {
                     const T *v_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + AG_TN * pitch) + lane * 4;
 #pragma unroll 8
-                    for (int j = 0; j < AG_TN; ++j) {
+                    for (int j = part * (AG_TN / with); j < (part + 1) * (AG_TN / with); ++j) {
                         const float4 e = reinterpret_cast<const float4 *>(w_s)[warp * AG_TN + j];
                         const float4 v4 = four(reinterpret_cast<const T *>(reinterpret_cast<const char *>(v_s) + j * pitch));
 #pragma unroll
@@ -153,10 +172,26 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
             __syncthreads();
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
+        if (with > 1) {   // the warps' sums over their tokens
+            if (lane * 4 < d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) *reinterpret_cast<float4 *>(x_s + (warp * 4 + r) * d + lane * 4) = make_float4(acc[r][0], acc[r][1], acc[r][2], acc[r][3]);
+            __syncthreads();
+            if (part == 0 && lane * 4 < d)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    for (int o = 1; o < with; ++o) {
+                        const float4 other = *reinterpret_cast<const float4 *>(x_s + ((warp + o) * 4 + r) * d + lane * 4);
+                        acc[r][0] += other.x;
+                        acc[r][1] += other.y;
+                        acc[r][2] += other.z;
+                        acc[r][3] += other.w;
+                    }
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int row = warp * 4 + r;
-            if (row >= rows) continue;
+            const int row = row_group * 4 + r;
+            if (row >= rows || part != 0) continue;
             if (g.slot < 0) {
                 if (lane * 4 < d) {
                     const int u = row_first + row;
@@ -210,13 +245,19 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mask_kernel(const AttnParams 
     }
 }
 
+__device__ __forceinline__ int run_of(long long tile, long long runs, long long total)
+{
+    return (int)times_over((tile + 1) * runs - 1, 1, total);
+}
+
 // The parts of a split unit, in the order of their tiles, to its rows: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
 // A thread has four components of a row; the threads of a CTA read neighbouring pieces of each part, which lie [M][d / 4] or, where a
 // thread of the kernel in front has a row (columns_first), [d / 4][M].  A unit that one run held is left alone.
 constexpr int AJ_THREADS = 128;
 template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_kernel(const AttnParams p, int M, int TN, int columns_first)
 {
-    wait_for_previous_kernel();
+    // (lengths and trees are as the kernel in front found them, which began behind everything that writes them: what follows from them is
+    // worked out while that one runs)
     const int lane = threadIdx.x & 31;
     const int units = p.h_kv * p.m_tiles, b = (int)blockIdx.x / units, head = (int)blockIdx.x % units / p.m_tiles, m_tile = (int)blockIdx.x % p.m_tiles;
     const int piece = (int)blockIdx.y * AJ_THREADS + (int)threadIdx.x, pieces = p.d / 4;
@@ -238,43 +279,60 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
         total += __shfl_xor_sync(0xffffffffu, total, off);
         before += __shfl_xor_sync(0xffffffffu, before, off);
     }
-    if (!fits) return;
-    const int row_first = m_tile * M, rows = min(M, s.rows * p.group - row_first);
-    if (rows <= 0) return;
+    // (no CTA ends before the kernel in front: what is behind this one must not overtake that)
+    const int row_first = m_tile * M, rows = fits ? min(M, s.rows * p.group - row_first) : 0;
+    if (rows <= 0) {
+        wait_for_previous_kernel();
+        return;
+    }
+    bool bad = false;
     if (p.row_offsets && p.parent) {
-        if (p.max_rows > AT_SMALL_ROWS) {
-            if (!p.tree_ok[b]) return;
-        } else {
-            bool bad = false;
+        if (p.max_rows > AT_SMALL_ROWS) bad = !p.tree_ok[b];
+        else {
             if ((int)threadIdx.x < s.rows) {
                 const int parent = p.parent[s.row0 + threadIdx.x];
                 bad = parent < -1 || parent >= (int)threadIdx.x;
             }
-            if (__syncthreads_or(bad)) return;
+            bad = __syncthreads_or(bad);
         }
     }
     const int tiles = attn_tiles(s, TN), m_tiles = (s.rows * p.group + M - 1) / M;
     const long long first = before + (long long)(head * m_tiles + m_tile) * tiles, last = first + tiles - 1;
     const long long runs = total < p.n_ctas ? total : p.n_ctas;
-    const int c0 = (int)(((first + 1) * runs - 1) / total), c1 = (int)(((last + 1) * runs - 1) / total);
-    if (c0 == c1 || row >= rows || column >= pieces) return;
+    // run c holds the tiles from total * c / runs on; of a tile, the last run that begins at it or in front of it
+    const int c0 = run_of(first, runs, total), c1 = run_of(last, runs, total);
+    wait_for_previous_kernel();
+    if (bad || c0 == c1 || row >= rows || column >= pieces) return;
 
     auto slot = [&](int c) { return (size_t)(c == c0 ? 2 * c + 1 : 2 * c); };
-    float m = -INFINITY;
-#pragma unroll 8
-    for (int c = c0; c <= c1; ++c) m = fmaxf(m, p.part_ml[(slot(c) * M + row) * 2]);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-#pragma unroll 8
-    for (int c = c0; c <= c1; ++c) {
-        const float2 ml = *reinterpret_cast<const float2 *>(p.part_ml + (slot(c) * M + row) * 2);
-        const float4 v = *reinterpret_cast<const float4 *>(p.part_o + (slot(c) * M * pieces + piece) * 4);
-        const float f = power_of_two(ml.x - ref);
-        l = fmaf(f, ml.y, l);
-        acc[0] = fmaf(f, v.x, acc[0]);
-        acc[1] = fmaf(f, v.y, acc[1]);
-        acc[2] = fmaf(f, v.z, acc[2]);
-        acc[3] = fmaf(f, v.w, acc[3]);
+    // eight parts at a time, their loads all on their way together
+    float m = -INFINITY, acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+    for (int c = c0; c <= c1; c += 8) {
+        float2 ml[8];
+        float4 v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const bool there = c + k <= c1;
+            ml[k] = there ? *reinterpret_cast<const float2 *>(p.part_ml + (slot(c + k) * M + row) * 2) : make_float2(-INFINITY, 0.f);
+            v[k] = there ? *reinterpret_cast<const float4 *>(p.part_o + (slot(c + k) * M * pieces + piece) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+        const float ref = top == -INFINITY ? 0.f : top, fade = power_of_two(m - ref);
+        m = top;
+        l *= fade;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] *= fade;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float f = power_of_two(ml[k].x - ref);
+            l = fmaf(f, ml[k].y, l);
+            acc[0] = fmaf(f, v[k].x, acc[0]);
+            acc[1] = fmaf(f, v[k].y, acc[1]);
+            acc[2] = fmaf(f, v[k].z, acc[2]);
+            acc[3] = fmaf(f, v[k].w, acc[3]);
+        }
     }
     const int u = row_first + row;
     T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + column * 4;
@@ -298,7 +356,10 @@ cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, bool
     return launch_behind(bf16 ? attn_join_kernel<__nv_bfloat16> : attn_join_kernel<float>, grid, AJ_THREADS, 0, stream, p, M, TN, columns_first ? 1 : 0);
 }
 
-AttnTiling attn_general_tiling() { return {AG_M, AG_TN, 3}; }
+AttnTiling attn_general_tiling(bool bf16, int d)
+{
+    return {AG_M, AG_TN, (bf16 ? ag_smem<__nv_bfloat16>(d) : ag_smem<float>(d)) <= (74 << 10) ? 3 : 2};
+}
 
 cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream)
 {
