@@ -22,6 +22,9 @@ template <typename T> constexpr size_t ag_smem(int d)
     return (size_t)AG_STAGES * 2 * AG_TN * ag_pitch<T>(d) + AG_M * d * sizeof(float) + 2 * AG_M * AG_TN * sizeof(float);
 }
 
+struct Yes { static constexpr bool value = true; };
+struct No { static constexpr bool value = false; };
+
 __device__ __forceinline__ float4 four(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 __device__ __forceinline__ float4 four(const __nv_bfloat16 *p)
 {
@@ -58,20 +61,32 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
         }
         if (p.row_offsets && kind == AT_WORDS && !p.tree_ok[g.b]) continue;
         const int row_first = g.m_tile * AG_M, rows = min(AG_M, g.s.rows * p.group - row_first);
-        for (int i = tid; i < rows * d; i += AG_THREADS) {
-            const int r = (row_first + i / d), node = r / p.group;
-            q_s[i] = load_as_float(static_cast<const T *>(p.q) + (size_t)(g.s.row0 + node) * p.q_stride +
-                                   (size_t)(g.head * p.group + r % p.group) * d + i % d);
+        for (int i = tid; i < rows * (d / 4); i += AG_THREADS) {
+            const int r = i / (d / 4), c = i % (d / 4) * 4, u = row_first + r, node = u / p.group;
+            *reinterpret_cast<float4 *>(q_s + r * d + c) = four(static_cast<const T *>(p.q) + (size_t)(g.s.row0 + node) * p.q_stride +
+                                                                (size_t)(g.head * p.group + u % p.group) * d + c);
         }
         const int with = rows <= 4 ? 4 : rows <= 8 ? 2 : 1, part = warp % with, row_group = warp / with;   // warps with the same rows
         // the last token that any of these rows sees: rows come in an order in which ancestors are in front
         const int last_node = (row_first + rows - 1) / p.group, upto = p.row_offsets ? g.s.len + last_node + 1 : g.s.len;
         const int tile1 = min(g.tile1, max((upto + AG_TN - 1) / AG_TN, g.tile0));
 
-        auto fetch = [&](int tile) {   // rows warp * 8 ... + 7 of the keys and of the values
+        // the page of this lane's token of a tile: asked for one tile ahead of the tile that is on its way
+        const int last_token = min(g.s.held, upto);
+        auto page_of = [&](int tile) {
+            const int t = tile * AG_TN + lane;
+            return tile < tile1 && t < last_token
+                       ? p.page_table[(size_t)g.b * p.max_pages + (p.page_shift >= 0 ? t >> p.page_shift : t / p.page_size)] : -1;
+        };
+        auto fetch = [&](int tile, int page) {   // rows warp * 8 ... + 7 of the keys and of the values
             if (tile < tile1) {
                 const uint32_t base = smem_u32(ag_smem_base) + (tile % AG_STAGES) * stage_bytes;
-                const long long mine = attn_token_offset(p, g.b, tile * AG_TN + lane, min(g.s.held, upto));
+                const int t = tile * AG_TN + lane;
+                long long mine = -1;
+                if (t < last_token) {
+                    if (page < 0 || page >= p.n_pages) report_status(p.status_dev, GDN_ERR_PAGE);
+                    else mine = page * p.page_stride + (p.page_shift >= 0 ? t & (p.page_size - 1) : t % p.page_size) * p.token_stride;
+                }
                 for (int r = warp * 8; r < warp * 8 + 8; ++r) {
                     const long long at = __shfl_sync(0xffffffffu, mine, r);
                     const long long from = (at < 0 ? 0 : at) + (long long)g.head * p.head_stride;
@@ -85,20 +100,26 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
 
+        // tokens that all rows of the unit see: in tiles of no others nothing is looked at token by token
+        const int common = !p.row_offsets ? upto : kind == AT_CHAIN ? g.s.len + row_first / p.group + 1 : g.s.len;
+        int node[4];
         float m[4], l[4], acc[4][4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
+            node[r] = (row_first + row_group * 4 + r) / p.group;
             m[r] = -INFINITY;
             l[r] = 0.f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[r][c] = 0.f;
         }
-        fetch(g.tile0);
+        int page = page_of(g.tile0 + 1);
+        fetch(g.tile0, page_of(g.tile0));
         for (int tile = g.tile0; tile < tile1; ++tile) {
-            fetch(tile + 1);
+            fetch(tile + 1, page);
+            page = page_of(tile + 2);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
             __syncthreads();
-            const bool busy = row_group * 4 < rows;
+            const bool busy = row_group * 4 < rows, clean = (tile + 1) * AG_TN <= common;
             float sc[4] = {0.f, 0.f, 0.f, 0.f};
             if (busy) {
                 const T *k_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + lane * pitch);
@@ -130,20 +151,16 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
                 float4 w;
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int row = row_group * 4 + r, node = (row_first + row) / p.group;
-                    const bool seen = row < rows && (t < g.s.len || (t < g.s.held && attn_sees(p, kind, anc, g.s.row0, node, t - g.s.len)));
+                    const bool seen = clean || (row_group * 4 + r < rows && (t < g.s.len || (t < g.s.held && attn_sees(p, kind, anc, g.s.row0, node[r], t - g.s.len))));
                     const float x = seen ? sc[r] * p.scale_log2 : -INFINITY;
                     float top = x;
 #pragma unroll
                     for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
                     top = fmaxf(top, m[r]);
                     const float ref = top == -INFINITY ? 0.f : top;
-                    const float e = seen ? exp2f(x - ref) : 0.f, fade = exp2f(m[r] - ref);
+                    const float e = seen ? power_of_two(x - ref) : 0.f, fade = power_of_two(m[r] - ref);
                     m[r] = top;
-                    float sum = e;
-#pragma unroll
-                    for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-                    l[r] = l[r] * fade + sum;
+                    l[r] = l[r] * fade + e;   // (of this lane's tokens)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) acc[r][c] *= fade;
                     (&w.x)[r] = e;
@@ -152,26 +169,35 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
                 __syncwarp();
                 if (lane * 4 < d) {
                     const T *v_s = reinterpret_cast<const T *>(ag_smem_base + (tile % AG_STAGES) * stage_bytes + AG_TN * pitch) + lane * 4;
-#pragma unroll 8
-                    for (int j = part * (AG_TN / with); j < (part + 1) * (AG_TN / with); ++j) {
+                    auto add = [&](int j, auto all) {
                         const float4 e = reinterpret_cast<const float4 *>(w_s)[warp * AG_TN + j];
                         const float4 v4 = four(reinterpret_cast<const T *>(reinterpret_cast<const char *>(v_s) + j * pitch));
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float er = (&e.x)[r];
-                            if (er != 0.f) {   // (a value that a row does not see may be infinite or no number)
+                            if (decltype(all)::value || er != 0.f) {   // (a value that a row does not see may be infinite or no number)
                                 acc[r][0] = fmaf(er, v4.x, acc[r][0]);
                                 acc[r][1] = fmaf(er, v4.y, acc[r][1]);
                                 acc[r][2] = fmaf(er, v4.z, acc[r][2]);
                                 acc[r][3] = fmaf(er, v4.w, acc[r][3]);
                             }
                         }
-                    }
+                    };
+                    const int from = part * (AG_TN / with), to = from + AG_TN / with;
+                    if (clean) {
+#pragma unroll 8
+                        for (int j = from; j < to; ++j) add(j, Yes{});
+                    } else
+                        for (int j = from; j < to; ++j) add(j, No{});
                 }
             }
             __syncthreads();
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int off = 16; off; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
         if (with > 1) {   // the warps' sums over their tokens
             if (lane * 4 < d)
 #pragma unroll

@@ -56,7 +56,7 @@ struct SampleShared {
     u64 table[32];                      // `powers`
     float table_4[32];                  // the same in units of 4
     u64 sorted[SA_SORT];                // rank 0: members of a bin
-    uint32_t count[SA_BINS];            // of the CTA; then, for the bins of this rank's share, of the cluster
+    uint32_t count[SA_BINS + 32];       // of the CTA; then, for the bins of this rank's share, of the cluster; 32 for what lies behind all bins
     u64 sum[2][3][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
     float top[SA_WARPS + 1];
     int best[SA_WARPS + 1];
@@ -362,7 +362,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float b = place_of((&v.x)[j]);
-                if (b < (float)SA_BINS) atomicAdd(&sh.count[(int)b], 1u);
+                atomicAdd(&sh.count[b < (float)SA_BINS ? (int)b : SA_BINS + lane], 1u);   // (behind the bins: no two lanes meet)
             }
         });
         cluster.sync();
