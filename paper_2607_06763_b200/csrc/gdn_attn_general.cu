@@ -36,12 +36,13 @@ __device__ __forceinline__ float4 four(const __nv_bfloat16 *p)
 // Four warps, each with four rows, or two or four of them with the same four where there are not enough: then each has a share of the
 // components in the products with the keys and of the tokens in those with the values.  A lane has a token in the former and four
 // components in the latter.  Bound by shared memory for many rows (a key's four components feed sixteen multiplications), by HBM for few.
-template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general_kernel(const AttnParams p)
+// DD: the components where they are known beforehand (64, 128), else 0.
+template <typename T, int DD> __global__ void __launch_bounds__(AG_THREADS, 3) attn_general_kernel(const AttnParams p)
 {
     extern __shared__ __align__(16) unsigned char ag_smem_base[];
     __shared__ unsigned long long anc[AT_SMALL_ROWS];
     __shared__ int anc_up[AT_SMALL_ROWS], tree_good;
-    const int d = p.d, pitch = ag_pitch<T>(d), stage_bytes = 2 * AG_TN * pitch;
+    const int d = DD ? DD : p.d, pitch = ag_pitch<T>(d), stage_bytes = 2 * AG_TN * pitch;
     float *q_s = reinterpret_cast<float *>(ag_smem_base + AG_STAGES * stage_bytes);
     float *x_s = reinterpret_cast<float *>(ag_smem_base);   // at the end, over the tiles: [4 warps][4 rows][d], sums of warps that share rows
     float *w_s = q_s + AG_M * d;        // [4 warps][AG_TN][4]: weights
@@ -87,13 +88,19 @@ template <typename T> __global__ void __launch_bounds__(AG_THREADS) attn_general
                     if (page < 0 || page >= p.n_pages) report_status(p.status_dev, GDN_ERR_PAGE);
                     else mine = page * p.page_stride + (p.page_shift >= 0 ? t & (p.page_size - 1) : t % p.page_size) * p.token_stride;
                 }
-                for (int r = warp * 8; r < warp * 8 + 8; ++r) {
-                    const long long at = __shfl_sync(0xffffffffu, mine, r);
-                    const long long from = (at < 0 ? 0 : at) + (long long)g.head * p.head_stride;
-                    if (lane * 16 < d * (int)sizeof(T)) {
-                        cp_async_16(base + r * pitch + lane * 16, reinterpret_cast<const char *>(k_cache + from) + lane * 16, at >= 0);
-                        cp_async_16(base + (AG_TN + r) * pitch + lane * 16, reinterpret_cast<const char *>(v_cache + from) + lane * 16,
-                                    at >= 0);
+                // 16-byte pieces of a row, and rows that an access of the warp covers
+                constexpr int PIECES = DD ? DD * (int)sizeof(T) / 16 : 32, ROWS = 32 / PIECES;
+                const int col = lane % PIECES;
+                const char *k_from = reinterpret_cast<const char *>(k_cache + g.head * p.head_stride) + col * 16;
+                const char *v_from = reinterpret_cast<const char *>(v_cache + g.head * p.head_stride) + col * 16;
+                mine *= (long long)sizeof(T);
+#pragma unroll
+                for (int h = 0; h < 8 / ROWS; ++h) {
+                    const int r = warp * 8 + h * ROWS + lane / PIECES;
+                    const long long at = __shfl_sync(0xffffffffu, mine, r), from = at < 0 ? 0 : at;
+                    if (DD || col * 16 < d * (int)sizeof(T)) {
+                        cp_async_16(base + r * pitch + col * 16, k_from + from, at >= 0);
+                        cp_async_16(base + (AG_TN + r) * pitch + col * 16, v_from + from, at >= 0);
                     }
                 }
             }
@@ -389,10 +396,16 @@ AttnTiling attn_general_tiling(bool bf16, int d)
 
 cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream)
 {
-    static PerContext seen[2];
-    const auto kernel = bf16 ? attn_general_kernel<__nv_bfloat16> : attn_general_kernel<float>;
+    // (bf16 with heads of 64 or 128 components has kernels of its own)
+    static PerContext seen[4];
+    using Kernel = void (*)(const AttnParams);
+    static const Kernel kernels[4] = {attn_general_kernel<__nv_bfloat16, 0>, attn_general_kernel<float, 0>, attn_general_kernel<float, 64>,
+                                      attn_general_kernel<float, 128>};
+    const int which = bf16 ? 0 : p.d == 64 ? 2 : p.d == 128 ? 3 : 1;
+    const Kernel kernel = kernels[which];
     int sms = 0;
-    const cudaError_t e = device_sms(seen[bf16], reinterpret_cast<const void *>(kernel), bf16 ? ag_smem<__nv_bfloat16>(GDN_MAX_HEAD_DIM) : ag_smem<float>(GDN_MAX_HEAD_DIM), &sms);
+    const cudaError_t e = device_sms(seen[which], reinterpret_cast<const void *>(kernel),
+                                     bf16 ? ag_smem<__nv_bfloat16>(GDN_MAX_HEAD_DIM) : ag_smem<float>(GDN_MAX_HEAD_DIM), &sms);
     if (e != cudaSuccess) return e;
     return launch_behind(kernel, dim3((unsigned)grid), AG_THREADS, bf16 ? ag_smem<__nv_bfloat16>(p.d) : ag_smem<float>(p.d), stream, p);
 }
