@@ -293,8 +293,7 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
     // worked out while that one runs)
     const int lane = threadIdx.x & 31;
     const int units = p.h_kv * p.m_tiles, b = (int)blockIdx.x / units, head = (int)blockIdx.x % units / p.m_tiles, m_tile = (int)blockIdx.x % p.m_tiles;
-    const int piece = (int)blockIdx.y * AJ_THREADS + (int)threadIdx.x, pieces = p.d / 4;
-    const int row = columns_first ? piece % M : piece / pieces, column = columns_first ? piece / M : piece % pieces;
+    const int pieces = p.d / 4;
     // the first tile of this unit among those of all units, as AttnWalk counts them
     AttnSeq s;
     const bool fits = attn_seq(p, b, s, false);
@@ -335,43 +334,47 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
     // run c holds the tiles from total * c / runs on; of a tile, the last run that begins at it or in front of it
     const int c0 = run_of(first, runs, total), c1 = run_of(last, runs, total);
     wait_for_previous_kernel();
-    if (bad || c0 == c1 || row >= rows || column >= pieces) return;
+    if (bad || c0 == c1) return;
 
     auto slot = [&](int c) { return (size_t)(c == c0 ? 2 * c + 1 : 2 * c); };
-    // eight parts at a time, their loads all on their way together
-    float m = -INFINITY, acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-    for (int c = c0; c <= c1; c += 8) {
-        float2 ml[8];
-        float4 v[8];
+    for (int piece = (int)blockIdx.y * AJ_THREADS + (int)threadIdx.x; piece < M * pieces; piece += (int)gridDim.y * AJ_THREADS) {
+        const int row = columns_first ? piece % M : piece / pieces, column = columns_first ? piece / M : piece % pieces;
+        if (row >= rows) continue;
+        // eight parts at a time, their loads all on their way together
+        float m = -INFINITY, acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+        for (int c = c0; c <= c1; c += 8) {
+            float2 ml[8];
+            float4 v[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const bool there = c + k <= c1;
-            ml[k] = there ? *reinterpret_cast<const float2 *>(p.part_ml + (slot(c + k) * M + row) * 2) : make_float2(-INFINITY, 0.f);
-            v[k] = there ? *reinterpret_cast<const float4 *>(p.part_o + (slot(c + k) * M * pieces + piece) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < 8; ++k) {
+                const bool there = c + k <= c1;
+                ml[k] = there ? *reinterpret_cast<const float2 *>(p.part_ml + (slot(c + k) * M + row) * 2) : make_float2(-INFINITY, 0.f);
+                v[k] = there ? *reinterpret_cast<const float4 *>(p.part_o + (slot(c + k) * M * pieces + piece) * 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            float top = m;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+            const float ref = top == -INFINITY ? 0.f : top, fade = power_of_two(m - ref);
+            m = top;
+            l *= fade;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] *= fade;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float f = power_of_two(ml[k].x - ref);
+                l = fmaf(f, ml[k].y, l);
+                acc[0] = fmaf(f, v[k].x, acc[0]);
+                acc[1] = fmaf(f, v[k].y, acc[1]);
+                acc[2] = fmaf(f, v[k].z, acc[2]);
+                acc[3] = fmaf(f, v[k].w, acc[3]);
+            }
         }
-        float top = m;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
-        const float ref = top == -INFINITY ? 0.f : top, fade = power_of_two(m - ref);
-        m = top;
-        l *= fade;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] *= fade;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const float f = power_of_two(ml[k].x - ref);
-            l = fmaf(f, ml[k].y, l);
-            acc[0] = fmaf(f, v[k].x, acc[0]);
-            acc[1] = fmaf(f, v[k].y, acc[1]);
-            acc[2] = fmaf(f, v[k].z, acc[2]);
-            acc[3] = fmaf(f, v[k].w, acc[3]);
-        }
+        const int u = row_first + row;
+        T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + column * 4;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+        else *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
     }
-    const int u = row_first + row;
-    T *o = static_cast<T *>(p.o) + ((size_t)(s.row0 + u / p.group) * p.h_q + head * p.group + u % p.group) * p.d + column * 4;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(o) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    else *reinterpret_cast<uint2 *>(o) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
 }
 
 }  // namespace
@@ -384,8 +387,10 @@ cudaError_t launch_attn_masks(const AttnParams &p, cudaStream_t stream)
 
 cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, bool columns_first, cudaStream_t stream)
 {
-    const int rows = columns_first ? M : min(M, p.max_rows * p.group);
-    const dim3 grid((unsigned)(p.n_seq * p.h_kv * p.m_tiles), (unsigned)((rows * (p.d / 4) + AJ_THREADS - 1) / AJ_THREADS));
+    // CTAs of a unit: one per 128 pieces of four components while that are fewer than eight per SM, else as many as make up those
+    const long long units = (long long)p.n_seq * p.h_kv * p.m_tiles, all = ((columns_first ? M : min(M, p.max_rows * p.group)) * (p.d / 4) + AJ_THREADS - 1) / AJ_THREADS;
+    const long long per_unit = max(1LL, min(all, 8LL * AT_SMS / units));
+    const dim3 grid((unsigned)units, (unsigned)per_unit);
     return launch_behind(bf16 ? attn_join_kernel<__nv_bfloat16> : attn_join_kernel<float>, grid, AJ_THREADS, 0, stream, p, M, TN, columns_first ? 1 : 0);
 }
 

@@ -9,8 +9,8 @@
 // overwrites S in tensor memory (128 columns of S and D of O per stream).  Maxima that rise by less than 2^8 do not move the sums:
 // weights up to 256 are as exact in bf16, and O is multiplied only where a row's maximum has risen by more.
 //
-// Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, warp 10 the products.
-// Two stages of keys and of values, each with its own barriers.  Pages whose size is a multiple of 8 come by tensor copies, a page
+// Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, which warp 11 looks at where
+// not all rows see them, warp 10 the products.  Two or more stages of keys and of values, each with its own barriers.  Pages whose size is a multiple of 8 come by tensor copies, a page
 // or a part of one each, straight into the swizzled layout of the products' operands; others by cp.async, row by row: one warp needs
 // 3300 clocks to issue a tile that way, the products of two streams 2048.
 // A row's 128 scores stay in its thread's registers (the warps of the rows take over what the others leave).
@@ -22,16 +22,20 @@ namespace gdn {
 namespace {
 
 constexpr int AS_THREADS = 384;
-constexpr int AS_M = 256, AS_TN = 128, AS_STAGES = 2;
+constexpr int AS_M = 256, AS_TN = 128, AS_MOST = 4;
 constexpr float AS_SLACK = 8.f;   // a maximum may rise by this many powers of two before the sums follow
 
 template <int D> __host__ __device__ constexpr int as_tile_bytes() { return AS_TN * D * 2; }
-template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t)as_tile_bytes<D>() * (2 + 2 * AS_STAGES) + 1024; }
+// Tiles of keys, and of values, on their way or at work: what shared memory holds beside the queries.  (With two of values, a tile's copy
+// of small pages, 4000 clocks, began too late: trees of 32 sequences 250 us instead of the present figure in the table.)
+template <int D> __host__ __device__ constexpr int as_k_stages() { return D == 128 ? 2 : 4; }
+template <int D> __host__ __device__ constexpr int as_v_stages() { return D == 128 ? 3 : 4; }
+template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t)as_tile_bytes<D>() * (2 + as_k_stages<D>() + as_v_stages<D>()) + 1024; }
 
 struct SplitShared {
     unsigned long long anc[AT_SMALL_ROWS];
     int anc_up[AT_SMALL_ROWS];
-    unsigned long long q_full, k_full[AS_STAGES], v_full[AS_STAGES], v_landed[AS_STAGES], k_empty[AS_STAGES], v_empty[AS_STAGES], s_full[2], p_full[2][2], o_full[2];   // p_full: [half of the tile][stream]
+    unsigned long long q_full, k_full[AS_MOST], v_full[AS_MOST], v_landed[AS_MOST], k_empty[AS_MOST], v_empty[AS_MOST], s_full[2], p_full[2][2], o_full[2];   // p_full: [half of the tile][stream]
     uint32_t tmem;
     int odd, dead, good;
 };
@@ -163,18 +167,18 @@ struct Unit {
 template <int D, bool TMA> __global__ void __launch_bounds__(AS_THREADS, 1)
 attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 {
-    constexpr int TILE = as_tile_bytes<D>(), KS = D / 16, PIECES = D / 8;
+    constexpr int TILE = as_tile_bytes<D>(), KS = D / 16, PIECES = D / 8, K_STAGES = as_k_stages<D>(), V_STAGES = as_v_stages<D>();
     extern __shared__ __align__(16) unsigned char as_raw[];
     __shared__ SplitShared sh;
     unsigned char *const data = as_raw + ((1024u - (smem_u32(as_raw) & 1023u)) & 1023u);   // swizzled tiles begin on 1024 bytes
-    const uint32_t q_s = smem_u32(data), k_s = q_s + 2 * TILE, v_s = k_s + AS_STAGES * TILE;
+    const uint32_t q_s = smem_u32(data), k_s = q_s + 2 * TILE, v_s = k_s + K_STAGES * TILE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = (int)blockIdx.x;
     const AttnMaskKind kind = attn_mask_kind(p);
     const __nv_bfloat16 *k_cache = static_cast<const __nv_bfloat16 *>(p.k_cache), *v_cache = static_cast<const __nv_bfloat16 *>(p.v_cache);
 
     if (tid == 0) {
         mbar_init(smem_u32(&sh.q_full), 8);
-        for (int i = 0; i < AS_STAGES; ++i) {
+        for (int i = 0; i < AS_MOST; ++i) {
             mbar_init(smem_u32(&sh.k_full[i]), 1);
             mbar_init(smem_u32(&sh.v_full[i]), 1);
             mbar_init(smem_u32(&sh.v_landed[i]), 1);
@@ -406,9 +410,25 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
         Unit t;
         while (next_unit(t)) {
             const AttnSegment &g = t.g;
+            // (by one warp) values of places that hold no token: zeros (their weights are 0, and 0 times what lies there may be no number);
+            // of tokens that not every row sees: what is infinite or no number is taken out, and added at the end of the unit
+            auto look_at_values = [&](int tile, uint32_t stage) {
+                if ((tile + 1) * AS_TN <= t.common) return;
+                for (int k = lane; k < AS_TN * PIECES; k += 32) {
+                    const int row = k / PIECES, token = tile * AS_TN + row;
+                    if (token < t.common) continue;
+                    uint4 *at = reinterpret_cast<uint4 *>(data + (v_s - q_s) + stage * TILE + as_at(row, k % PIECES));
+                    uint4 y = *at;
+                    if (token >= t.upto) *at = make_uint4(0, 0, 0, 0);
+                    else if (zero_odd(y)) {
+                        *at = y;
+                        sh.odd = 1;
+                    }
+                }
+            };
             if (warp < 10) {   // ---- tiles, of keys or of values
                 const bool keys = warp == 8;
-                const uint32_t to = keys ? k_s : v_s;
+                const uint32_t to = keys ? k_s : v_s, stages = keys ? K_STAGES : V_STAGES;
                 unsigned long long *full = keys ? sh.k_full : sh.v_full, *empty = keys ? sh.k_empty : sh.v_empty;
                 constexpr int ASKS = TMA ? 1 : 4;   // places that a lane looks up: of its box, or of four tokens
                 const int box = TMA ? maps.box : 1;
@@ -424,8 +444,8 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                 };
                 ask(g.tile0);
                 for (int i = 0; i < t.n_tiles; ++i) {
-                    const uint32_t n = done + i;
-                    const int stage = n % AS_STAGES, tile = g.tile0 + i;
+                    const uint32_t n = done + i, stage = n % stages;
+                    const int tile = g.tile0 + i;
                     bool good[ASKS];
                     int in_page[ASKS], at_page[ASKS];
 #pragma unroll
@@ -438,7 +458,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         in_page[k] = p.page_shift >= 0 ? token & (p.page_size - 1) : token % p.page_size;
                     }
                     ask(tile + 1);
-                    if (n >= AS_STAGES && !wait(&empty[stage], (n / AS_STAGES - 1) & 1)) break;
+                    if (n >= stages && !wait(&empty[stage], (n / stages - 1) & 1)) break;
                     if constexpr (TMA) {
                         const uint32_t bar = smem_u32(keys ? &sh.k_full[stage] : &sh.v_landed[stage]);
                         if (lane == 0) mbar_expect_tx(bar, TILE);
@@ -448,7 +468,6 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                             for (int c = 0; c < D / 64; ++c)
                                 tma_load_4d(to + stage * TILE + c * (AS_TN * 128) + lane * box * 128, keys ? &maps.k : &maps.v, c * 64, in_page[0], g.head,
                                             good[0] ? at_page[0] : p.n_pages, bar);
-                        if (!keys && !wait(&sh.v_landed[stage], (n / AS_STAGES) & 1)) break;
                     } else {
                         constexpr int ROWS = 32 / PIECES;   // rows that one access of the warp covers
                         const int col = lane % PIECES;
@@ -466,32 +485,25 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         cp_async_wait_all();
                         __syncwarp();
                     }
-                    // values of places that hold no token: zeros (their weights are 0, and 0 times what lies there may be no number); of tokens that
-                    // not every row sees: what is infinite or no number is taken out, and added at the end of the unit
-                    if (!keys && (tile + 1) * AS_TN > t.common) {
-                        for (int k = lane; k < AS_TN * PIECES; k += 32) {
-                            const int row = k / PIECES, token = tile * AS_TN + row;
-                            if (token < t.common) continue;
-                            uint4 *at = reinterpret_cast<uint4 *>(data + (v_s - q_s) + stage * TILE + as_at(row, k % PIECES));
-                            uint4 y = *at;
-                            if (token >= t.upto) *at = make_uint4(0, 0, 0, 0);
-                            else if (zero_odd(y)) {
-                                *at = y;
-                                sh.odd = 1;
-                            }
-                        }
-                        __syncwarp();
-                    }
-                    if (!TMA || !keys) {
+                    if constexpr (!TMA) {
+                        if (!keys) look_at_values(tile, stage);
                         fence_proxy_async();
                         mbar_arrive_warp(smem_u32(&full[stage]), lane);
                     }
+                }
+            } else if (TMA && warp == 11) {   // ---- values that have landed
+                for (int i = 0; i < t.n_tiles; ++i) {
+                    const uint32_t n = done + i, stage = n % V_STAGES;
+                    if (!wait(&sh.v_landed[stage], (n / V_STAGES) & 1)) break;
+                    look_at_values(g.tile0 + i, stage);
+                    fence_proxy_async();
+                    mbar_arrive_warp(smem_u32(&sh.v_full[stage]), lane);
                 }
             } else if (warp == 10 && t.n_tiles > 0) {   // ---- products, by one thread: what it does between two of them the tensor cores may wait for
                 if (elect_one()) {
                     constexpr uint32_t id_s = idesc_bf16(128, 128), id_o = idesc_bf16(128, D) | (1u << 16);
                     auto scores = [&](int s, uint32_t n) {
-                        const uint64_t q_d = smem_desc_sw128(q_s + s * TILE), k_d = smem_desc_sw128(k_s + (n % AS_STAGES) * TILE);
+                        const uint64_t q_d = smem_desc_sw128(q_s + s * TILE), k_d = smem_desc_sw128(k_s + (n % K_STAGES) * TILE);
 #pragma unroll
                         for (int k = 0; k < KS; ++k) {
                             const uint64_t on = ((k >> 2) * (AS_TN * 128) + (k & 3) * 32) >> 4;
@@ -499,18 +511,18 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         }
                         umma_commit(smem_u32(&sh.s_full[s]));
                     };
-                    bool ok = wait_alone(&sh.q_full, units & 1) && wait_alone(&sh.k_full[done % AS_STAGES], (done / AS_STAGES) & 1);
+                    bool ok = wait_alone(&sh.q_full, units & 1) && wait_alone(&sh.k_full[done % K_STAGES], (done / K_STAGES) & 1);
                     tc_fence_after();
                     if (ok) {
                         for (int s = 0; s < t.streams; ++s) scores(s, done);
-                        umma_commit(smem_u32(&sh.k_empty[done % AS_STAGES]));
+                        umma_commit(smem_u32(&sh.k_empty[done % K_STAGES]));
                     }
                     for (int i = 0; i < t.n_tiles && ok; ++i) {
                         const uint32_t n = done + i, next = n + 1;
-                        const int stage = n % AS_STAGES;
+                        const uint32_t stage = n % V_STAGES;
                         const uint64_t v_d = desc_rows_along_k(v_s + stage * TILE);
                         const bool more = i + 1 < t.n_tiles;
-                        ok = wait_alone(&sh.v_full[stage], (n / AS_STAGES) & 1);
+                        ok = wait_alone(&sh.v_full[stage], (n / V_STAGES) & 1);
                         for (int s = 0; s < t.streams && ok; ++s) {
 #pragma unroll
                             for (int half = 0; half < 2; ++half) {
@@ -527,7 +539,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                             if (!more) umma_commit(smem_u32(&sh.o_full[s]));
                             else {
                                 if (s == 0) {
-                                    ok = wait_alone(&sh.k_full[next % AS_STAGES], (next / AS_STAGES) & 1);
+                                    ok = wait_alone(&sh.k_full[next % K_STAGES], (next / K_STAGES) & 1);
                                     tc_fence_after();
                                 }
                                 if (ok) scores(s, next);
@@ -535,7 +547,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                         }
                         if (ok) {
                             umma_commit(smem_u32(&sh.v_empty[stage]));
-                            if (more) umma_commit(smem_u32(&sh.k_empty[next % AS_STAGES]));
+                            if (more) umma_commit(smem_u32(&sh.k_empty[next % K_STAGES]));
                         }
                     }
                 }
