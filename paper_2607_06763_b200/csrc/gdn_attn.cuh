@@ -33,7 +33,7 @@ struct AttnParams {
     int mask_words;
     int32_t *tree_ok;                                // [n_seq]
     float *part_o, *part_ml;                         // [2 * CTAs][M * d], [2 * CTAs][M][2]: sums; maximum, denominator
-    int n_ctas;
+    int n_ctas, over;                                // runs; tiles that a unit counts for beyond its own
 };
 
 struct AttnLayout {
@@ -91,10 +91,10 @@ struct AttnSegment {
 
 __device__ __forceinline__ int attn_tiles(const AttnSeq &s, int TN) { return s.held > TN ? (s.held + TN - 1) / TN : 1; }
 
-__device__ __forceinline__ long long attn_seq_work(const AttnParams &p, int b, int M, int TN, AttnSeq &s, bool report)
+// Units of sequence b, each of attn_tiles(s, TN) tiles; 0 where its lengths are not possible.
+__device__ __forceinline__ int attn_units(const AttnParams &p, int b, int M, AttnSeq &s, bool report)
 {
-    if (!attn_seq(p, b, s, report)) return 0;
-    return (long long)p.h_kv * ((s.rows * p.group + M - 1) / M) * attn_tiles(s, TN);
+    return attn_seq(p, b, s, report) ? p.h_kv * ((s.rows * p.group + M - 1) / M) : 0;
 }
 
 // a * b / c, by a 32-bit division wherever the product fits (a 64-bit one takes some hundred instructions).
@@ -115,11 +115,47 @@ __device__ __forceinline__ long long warp_scan(long long x, int lane)
     return x;
 }
 
+// What all runs together hold, and what of it lies in the sequences of this lane and in front of sequence `before_b`, by a whole warp.
+struct AttnTotal {
+    long long total, mine, before;
+    int over;   // tiles that a unit counts for beyond its own
+};
+__device__ __forceinline__ AttnTotal attn_total(const AttnParams &p, int M, int TN, int before_b, bool report)
+{
+    const int lane = threadIdx.x & 31, per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
+    long long tiles = 0, units = 0, tiles_before = 0, units_before = 0;
+    for (int i = b0; i < b1; ++i) {
+        AttnSeq s;
+        const int n = attn_units(p, i, M, s, report);
+        const long long t = n ? (long long)n * attn_tiles(s, TN) : 0;
+        tiles += t;
+        units += n;
+        if (i < before_b) {
+            tiles_before += t;
+            units_before += n;
+        }
+    }
+    long long all_tiles = tiles, all_units = units;
+#pragma unroll
+    for (int off = 16; off; off >>= 1) {
+        all_tiles += __shfl_xor_sync(0xffffffffu, all_tiles, off);
+        all_units += __shfl_xor_sync(0xffffffffu, all_units, off);
+        tiles_before += __shfl_xor_sync(0xffffffffu, tiles_before, off);
+        units_before += __shfl_xor_sync(0xffffffffu, units_before, off);
+    }
+    AttnTotal r;
+    r.over = all_tiles >= 4ll * p.n_ctas ? p.over : 0;
+    r.total = all_tiles + all_units * r.over;
+    r.mine = tiles + units * r.over;
+    r.before = tiles_before + units_before * r.over;
+    return r;
+}
+
 // The run of one CTA, walked by every warp on its own (the same values in all of them; no exchange between warps).
 struct AttnWalk {
-    long long at, end;   // tiles of the run, counted over all units
-    long long seq_at;    // the first tile of sequence b
-    int b;
+    long long at, end;   // the run, counted over all units
+    long long seq_at;    // where sequence b begins
+    int b, over;
     AttnSeq s;
 
     __device__ __forceinline__ void begin(const AttnParams &p, int cta, int M, int TN)
@@ -131,12 +167,9 @@ struct AttnWalk {
         }
         const int lane = threadIdx.x & 31;
         const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
-        long long mine = 0;
-        for (int i = b0; i < b1; ++i) {
-            AttnSeq t;
-            mine += attn_seq_work(p, i, M, TN, t, cta == 0 && threadIdx.x < 32);
-        }
-        const long long upto = warp_scan(mine, lane), total = __shfl_sync(0xffffffffu, upto, 31);
+        const AttnTotal sum = attn_total(p, M, TN, 0, cta == 0 && threadIdx.x < 32);
+        const long long mine = sum.mine, upto = warp_scan(mine, lane), total = sum.total;
+        over = sum.over;
         const long long runs = total < p.n_ctas ? total : p.n_ctas;
         at = end = 0;
         if (cta >= runs) return;
@@ -150,7 +183,8 @@ struct AttnWalk {
         if (lane == owner)
             for (int i = b0; i < b1; ++i) {
                 AttnSeq t;
-                const long long w = attn_seq_work(p, i, M, TN, t, false);
+                const int n = attn_units(p, i, M, t, false);
+                const long long w = n ? (long long)n * (attn_tiles(t, TN) + over) : 0;
                 if (begins + w > at) {
                     found = i;
                     break;
@@ -176,24 +210,30 @@ struct AttnWalk {
             g.tile1 = g.tiles = attn_tiles(g.s, TN);
             return true;
         }
-        for (;;) {   // ends: tile `at` of the `total` belongs to some sequence
-            const long long w = attn_seq_work(p, b, M, TN, s, false);
-            if (at < seq_at + w) break;
-            seq_at += w;
-            ++b;
-        }
-        g.s = s;
-        g.b = b;
-        g.tiles = attn_tiles(s, TN);
-        const int unit = (int)times_over(at - seq_at, 1, g.tiles);
-        const int m_tiles = (s.rows * p.group + M - 1) / M;
-        g.head = unit / m_tiles;
-        g.m_tile = unit % m_tiles;
-        g.tile0 = (int)((at - seq_at) - (long long)unit * g.tiles);
-        const long long left = end - at;
-        g.tile1 = left < g.tiles - g.tile0 ? g.tile0 + (int)left : g.tiles;
+        do {   // (what a unit counts for beyond its tiles is no work)
+            if (at >= end) return false;
+            for (;;) {   // place `at` of the total belongs to some sequence
+                if (b >= p.n_seq) return false;   // (lengths that changed meanwhile)
+                const int n = attn_units(p, b, M, s, false);
+                const long long w = n ? (long long)n * (attn_tiles(s, TN) + over) : 0;
+                if (at < seq_at + w) break;
+                seq_at += w;
+                ++b;
+            }
+            g.s = s;
+            g.b = b;
+            g.tiles = attn_tiles(s, TN);
+            const int per = g.tiles + over, unit = (int)times_over(at - seq_at, 1, per), m_tiles = (s.rows * p.group + M - 1) / M;
+            g.head = unit / m_tiles;
+            g.m_tile = unit % m_tiles;
+            const int from = (int)((at - seq_at) - (long long)unit * per);
+            const long long left = end - at;
+            const int to = left < per - from ? from + (int)left : per;
+            g.tile0 = max(from - over, 0);
+            g.tile1 = max(to - over, 0);
+            at += to - from;
+        } while (g.tile0 == g.tile1);
         g.slot = g.tile0 == 0 ? (g.tile1 == g.tiles ? -1 : 2 * cta + 1) : 2 * cta;
-        at += g.tile1 - g.tile0;
         return true;
     }
 };
@@ -269,7 +309,7 @@ __device__ __forceinline__ AttnMaskKind attn_mask_kind(const AttnParams &p)
 
 constexpr int AT_SMS = 148;
 struct AttnTiling {
-    int M, TN, ctas;   // rows and tokens of a tile, CTAs that an SM holds
+    int M, TN, ctas, over;   // rows and tokens of a tile, CTAs that an SM holds, tiles that take as long as what a unit takes beside its own
 };
 AttnTiling attn_general_tiling(bool bf16, int d);
 // `bf16`: the type of rows, cache and outputs; otherwise fp32.

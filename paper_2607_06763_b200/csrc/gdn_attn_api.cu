@@ -119,6 +119,7 @@ int attention(const gdn_attn_shape_t *shape, const void *q, const void *k_cache,
     p.part_o = reinterpret_cast<float *>(w + c.layout.part_o);
     p.part_ml = reinterpret_cast<float *>(w + c.layout.part_ml);
     p.n_ctas = c.grid;
+    p.over = c.tiling.over;
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     const bool bf16 = s.dtype == GDN_BF16;
     if (parent && s.max_rows > AT_SMALL_ROWS && launch_attn_masks(p, stream) != cudaSuccess) return GDN_ERR_CUDA;

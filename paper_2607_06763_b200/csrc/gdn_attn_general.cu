@@ -291,26 +291,12 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
 {
     // (lengths and trees are as the kernel in front found them, which began behind everything that writes them: what follows from them is
     // worked out while that one runs)
-    const int lane = threadIdx.x & 31;
     const int units = p.h_kv * p.m_tiles, b = (int)blockIdx.x / units, head = (int)blockIdx.x % units / p.m_tiles, m_tile = (int)blockIdx.x % p.m_tiles;
     const int pieces = p.d / 4;
     // the first tile of this unit among those of all units, as AttnWalk counts them
     AttnSeq s;
     const bool fits = attn_seq(p, b, s, false);
-    const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
-    long long mine = 0, before = 0;
-    for (int i = b0; i < b1; ++i) {
-        AttnSeq t;
-        const long long w = attn_seq_work(p, i, M, TN, t, false);
-        mine += w;
-        if (i < b) before += w;
-    }
-    long long total = mine;
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        total += __shfl_xor_sync(0xffffffffu, total, off);
-        before += __shfl_xor_sync(0xffffffffu, before, off);
-    }
+    const AttnTotal sum = attn_total(p, M, TN, b, false);
     // (no CTA ends before the kernel in front: what is behind this one must not overtake that)
     const int row_first = m_tile * M, rows = fits ? min(M, s.rows * p.group - row_first) : 0;
     if (rows <= 0) {
@@ -329,9 +315,9 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
         }
     }
     const int tiles = attn_tiles(s, TN), m_tiles = (s.rows * p.group + M - 1) / M;
-    const long long first = before + (long long)(head * m_tiles + m_tile) * tiles, last = first + tiles - 1;
-    const long long runs = total < p.n_ctas ? total : p.n_ctas;
-    // run c holds the tiles from total * c / runs on; of a tile, the last run that begins at it or in front of it
+    const long long first = sum.before + (long long)(head * m_tiles + m_tile) * (tiles + sum.over) + sum.over, last = first + tiles - 1;
+    const long long total = sum.total, runs = total < p.n_ctas ? total : p.n_ctas;
+    // run c begins at total * c / runs; a tile's is the last that begins at it or in front of it
     const int c0 = run_of(first, runs, total), c1 = run_of(last, runs, total);
     wait_for_previous_kernel();
     if (bad || c0 == c1) return;
@@ -396,7 +382,7 @@ cudaError_t launch_attn_join(const AttnParams &p, bool bf16, int M, int TN, bool
 
 AttnTiling attn_general_tiling(bool bf16, int d)
 {
-    return {AG_M, AG_TN, (bf16 ? ag_smem<__nv_bfloat16>(d) : ag_smem<float>(d)) <= (74 << 10) ? 3 : 2};
+    return {AG_M, AG_TN, (bf16 ? ag_smem<__nv_bfloat16>(d) : ag_smem<float>(d)) <= (74 << 10) ? 3 : 2, 2};
 }
 
 cudaError_t launch_attn_general(const AttnParams &p, bool bf16, int grid, cudaStream_t stream)

@@ -316,7 +316,7 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
 
 AttnTiling attn_rows_tiling(int rows, int d)
 {
-    return {rows <= 16 ? 16 : rows <= 32 ? 32 : 64, AR_TN, d == 128 ? ar_ctas<128>() : ar_ctas<64>()};
+    return {rows <= 16 ? 16 : rows <= 32 ? 32 : 64, AR_TN, d == 128 ? ar_ctas<128>() : ar_ctas<64>(), 2};
 }
 
 cudaError_t launch_attn_rows(const AttnParams &p, int M, int grid, cudaStream_t stream)
