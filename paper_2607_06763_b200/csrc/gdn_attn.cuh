@@ -115,12 +115,19 @@ __device__ __forceinline__ long long warp_scan(long long x, int lane)
     return x;
 }
 
+// Sum over the lanes of numbers below 2^50, by two reductions of 32 bits.
+__device__ __forceinline__ long long warp_sum(long long x)
+{
+    const uint32_t lo = (uint32_t)x & 0xFFFFFFu, hi = (uint32_t)(x >> 24);
+    return ((long long)__reduce_add_sync(0xffffffffu, hi) << 24) + __reduce_add_sync(0xffffffffu, lo);
+}
+
 // What all runs together hold, and what of it lies in the sequences of this lane and in front of sequence `before_b`, by a whole warp.
 struct AttnTotal {
     long long total, mine, before;
     int over;   // tiles that a unit counts for beyond its own
 };
-__device__ __forceinline__ AttnTotal attn_total(const AttnParams &p, int M, int TN, int before_b, bool report)
+template <bool BEFORE> __device__ __forceinline__ AttnTotal attn_total(const AttnParams &p, int M, int TN, int before_b, bool report)
 {
     const int lane = threadIdx.x & 31, per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
     long long tiles = 0, units = 0, tiles_before = 0, units_before = 0;
@@ -135,19 +142,12 @@ __device__ __forceinline__ AttnTotal attn_total(const AttnParams &p, int M, int 
             units_before += n;
         }
     }
-    long long all_tiles = tiles, all_units = units;
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        all_tiles += __shfl_xor_sync(0xffffffffu, all_tiles, off);
-        all_units += __shfl_xor_sync(0xffffffffu, all_units, off);
-        tiles_before += __shfl_xor_sync(0xffffffffu, tiles_before, off);
-        units_before += __shfl_xor_sync(0xffffffffu, units_before, off);
-    }
+    const long long all_tiles = warp_sum(tiles), all_units = __reduce_add_sync(0xffffffffu, (uint32_t)units);
     AttnTotal r;
     r.over = all_tiles >= 4ll * p.n_ctas ? p.over : 0;
     r.total = all_tiles + all_units * r.over;
     r.mine = tiles + units * r.over;
-    r.before = tiles_before + units_before * r.over;
+    r.before = BEFORE ? warp_sum(tiles_before + units_before * r.over) : 0;
     return r;
 }
 
@@ -167,7 +167,7 @@ struct AttnWalk {
         }
         const int lane = threadIdx.x & 31;
         const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
-        const AttnTotal sum = attn_total(p, M, TN, 0, cta == 0 && threadIdx.x < 32);
+        const AttnTotal sum = attn_total<false>(p, M, TN, 0, cta == 0 && threadIdx.x < 32);
         const long long mine = sum.mine, upto = warp_scan(mine, lane), total = sum.total;
         over = sum.over;
         const long long runs = total < p.n_ctas ? total : p.n_ctas;

@@ -296,7 +296,7 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
     // the first tile of this unit among those of all units, as AttnWalk counts them
     AttnSeq s;
     const bool fits = attn_seq(p, b, s, false);
-    const AttnTotal sum = attn_total(p, M, TN, b, false);
+    const AttnTotal sum = attn_total<true>(p, M, TN, b, false);
     // (no CTA ends before the kernel in front: what is behind this one must not overtake that)
     const int row_first = m_tile * M, rows = fits ? min(M, s.rows * p.group - row_first) : 0;
     if (rows <= 0) {

@@ -582,7 +582,7 @@ bool cache_map(CUtensorMap *tm, const void *cache, const AttnParams &p, int box)
 
 }  // namespace
 
-AttnTiling attn_sm100_tiling() { return {AS_M, AS_TN, 1, 2}; }
+AttnTiling attn_sm100_tiling() { return {AS_M, AS_TN, 1, 4}; }
 
 cudaError_t launch_attn_sm100(const AttnParams &p, int grid, cudaStream_t stream)
 {
