@@ -10,8 +10,8 @@
 // many CTAs an SM holds; the rows at work at one time are some 100 MB at most).  Nothing is sorted but the
 // members of one bin: (m - x) / T in units of 1/32 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
 // The first k end in a bin that the counts tell.  Where the p end the counts nearly tell: a count times the weight at the bin's middle
-// is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, inside it and
-// altogether, and sees whether it is the one (else the estimate starts again from these sums).  Only that bin's members (some hundreds
+// is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, in it and
+// its neighbours, and altogether, and sees whether it is one of the three (else the estimate starts again from these sums).  Only that bin's members (some hundreds
 // of 131071) are put in order; a bin with more members than fit (many equal logits) is bisected instead.  What the pass summed up
 // to the bin, warp by warp, also says where the token lies.
 // The first k of a row, k up to a thousand, are put in order at once, and the row is done with.
@@ -57,7 +57,7 @@ struct SampleShared {
     float table_4[32];                  // the same in units of 4
     u64 sorted[SA_SORT];                // rank 0: members of a bin
     uint32_t count[SA_BINS + 32];       // of the CTA; then, for the bins of this rank's share, of the cluster; 32 for what lies behind all bins
-    u64 sum[2][3][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
+    u64 sum[2][4][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
     float top[SA_WARPS + 1];
     int best[SA_WARPS + 1];
     int members;                        // rank 0: entries of `sorted`
@@ -319,15 +319,18 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     auto place_of = [&](float x) { return (m - x) * to_bin; };   // its whole part is the bin; it falls as x rises (no number: in no bin)
 
     int turn = 0;
-    // sums of three numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
-    auto cluster_sum = [&](u64 (&a)[3], u64 (&all)[3], u64 *before) {
+    // sums of up to four numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
+    auto cluster_sum = [&](auto &a, auto &all, u64 *before) {
+        constexpr int N = (int)(sizeof(a) / sizeof(u64));
 #pragma unroll
         for (int off = 16; off; off >>= 1)
 #pragma unroll
-            for (int i = 0; i < 3; ++i) a[i] += __shfl_xor_sync(0xffffffffu, a[i], off);
-        if (lane < 3) sh.sum[turn][lane][warp] = lane == 0 ? a[0] : lane == 1 ? a[1] : a[2];
+            for (int i = 0; i < N; ++i) a[i] += __shfl_xor_sync(0xffffffffu, a[i], off);
+        if (lane == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sh.sum[turn][i][warp] = a[i];
         __syncthreads();
-        if (tid < 3) {
+        if (tid < N) {
             u64 s = 0;
             for (int i = 0; i < SA_WARPS; ++i) s += sh.sum[turn][tid][i];
             sh.sum[turn][tid][SA_WARPS] = s;
@@ -335,10 +338,10 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
         cluster.sync();
         u64 front = 0;
 #pragma unroll
-        for (int i = 0; i < 3; ++i) all[i] = 0;
+        for (int i = 0; i < N; ++i) all[i] = 0;
         for (int r = 0; r < ranks; ++r) {
 #pragma unroll
-            for (int i = 0; i < 3; ++i) all[i] += *cluster.map_shared_rank(&sh.sum[turn][i][SA_WARPS], r);
+            for (int i = 0; i < N; ++i) all[i] += *cluster.map_shared_rank(&sh.sum[turn][i][SA_WARPS], r);
             if (before && r + 1 == rank) front = all[0];
         }
         if (before) {
@@ -453,7 +456,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                 u64 lo = 0, hi = ~0ull;
                 while (lo < hi) {
                     const u64 mid = lo + (hi - lo) / 2;
-                    u64 a[3] = {0, 0, 0}, all[3];
+                    u64 a[2] = {0, 0}, all[2];
                     each(from_place, to_place, [&](const float4 &v, int i) {
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
@@ -637,8 +640,9 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
             bool found = false;
             u64 up = 0, z = 0;
             while (bin >= 0) {   // ends: the bins between low and high get fewer
-                u64 a[3] = {0, 0, 0}, all[3], keep = 0;   // up to the bin, inside it, all of the prefix
-                const float to = (float)bin, behind = (float)(bin + 1);
+                // the weights up to the bin in front of this one, in that one, in this one and in the next; of all of the prefix
+                u64 a[4] = {0, 0, 0, 0}, all[4], z_own[1] = {0}, z_all[1], keep[3] = {0, 0, 0};
+                const float to = (float)(bin - 1), this_one = (float)bin, next = (float)(bin + 1), behind = (float)(bin + 2);
                 each(from_place, to_place, [&](const float4 &v, int i) {
                     u64 w4[4];
                     weigh.four(v, w4);
@@ -646,45 +650,61 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                     for (int j = 0; j < 4; ++j) {
                         const float x = (&v.x)[j], b = place_of(x);
                         if (by_k && !inside(b, x, i + j)) continue;
-                        a[2] += w4[j];
+                        z_own[0] += w4[j];
                         if (b < to) {
                             a[0] += w4[j];
-                            if (least && w4[j] >= least) keep += w4[j];
+                            if (least && w4[j] >= least) keep[0] += w4[j];
                         } else if (b < behind) {
-                            a[1] += w4[j];
-                            gather(b, x, i + j, bin);
+                            const u64 kept = w4[j] >= least ? w4[j] : 0;
+                            if (b < this_one) {
+                                a[1] += w4[j];
+                                keep[1] += kept;
+                            } else if (b < next) {
+                                a[2] += w4[j];
+                                keep[2] += kept;
+                                gather(b, x, i + j, bin);
+                            } else
+                                a[3] += w4[j];
                         }
                     }
                 });
-                if (!least) keep = a[0];
+                if (!least) keep[0] = a[0];
                 cluster_sum(a, all, nullptr);
-                up = all[0];
-                z = all[2];
+                cluster_sum(z_own, z_all, nullptr);
+                z = z_all[0];
                 const double goal = (double)top_p * (double)z;
-                if (up > 0 && (double)up >= goal) high = bin;                          // it ends in front of the bin
-                else if ((double)(up + all[1]) < goal) low = bin;                      // or behind it
+                const u64 to1 = all[0] + all[1], to2 = to1 + all[2], to3 = to2 + all[3];
+                if (all[0] > 0 && (double)all[0] >= goal) high = bin - 1;             // it ends further in front
+                else if ((double)to3 < goal) low = bin + 1;                            // or further behind
                 else {
                     found = true;
-                    w = keep;
+                    // (an empty prefix is never enough)
+                    const int step = to1 > 0 && (double)to1 >= goal ? -1 : to2 > 0 && (double)to2 >= goal ? 0 : 1;
+                    up = step < 0 ? all[0] : step == 0 ? to1 : to2;
+                    w = keep[0] + (step >= 0 ? keep[1] : 0) + (step > 0 ? keep[2] : 0);
+                    if (step != 0) {
+                        bin += step;
+                        empty_list();
+                        each_short(from_place, to_place, [&](const float4 &v, int i) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) gather(place_of((&v.x)[j]), (&v.x)[j], i + j, bin);
+                        });
+                        cluster.sync();
+                    }
                     break;
                 }
                 empty_list();
                 // the estimate again, from the sums that are now known: the threads' prefix sums are compared with a goal that is moved
-                if (tid == bin / SA_OWN) {
-                    float a = ab;
+                if (tid == max(bin - 1, 0) / SA_OWN) {
+                    float e = ab;
 #pragma unroll
                     for (int j = 0; j < SA_OWN; ++j) {
-                        if (j == bin % SA_OWN) {
-                            sh.scan_a[0] = a;                                          // estimated up to the bin
-                            sh.scan_a[1] = about[j];
-                        }
-                        a += about[j];
+                        if (j == max(bin - 1, 0) % SA_OWN) sh.scan_a[0] = e;           // estimated up to the bin in front
+                        e += about[j];
                     }
                 }
                 __syncthreads();
-                const float moved = high == bin ? (float)(goal - (double)up) + sh.scan_a[0]
-                                                : (float)(goal - (double)(up + all[1])) + sh.scan_a[0] + sh.scan_a[1];
-                bin = search(low, high, moved);
+                bin = search(low, high, (float)(goal - (double)all[0]) + sh.scan_a[0]);
             }
             if (found) {
                 const double goal = (double)top_p * (double)z;
@@ -744,7 +764,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
 #pragma unroll
             for (int j = 0; j < 4; ++j) w += own[j];
         });
-    u64 sums[3] = {w, 0, 0}, all[3], before;
+    u64 sums[1] = {w}, all[1], before;
     cluster_sum(sums, all, &before);
     const u64 z = all[0];
     double u = (double)p.uniform[row];
