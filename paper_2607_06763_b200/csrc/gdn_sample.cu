@@ -17,8 +17,8 @@
 // The first k of a row, k up to a thousand, are put in order at once, and the row is done with.
 //
 // A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-38 (no order
-// of additions matters).  Those of 2^-6 and more are formed to about 1e-9 of themselves, the others to fp32: their errors are as often
-// up as down, and 2^-30 at most.  The difference m - x is kept in two parts, and so is 1 / T.  Tokens more than 39 powers of two
+// of additions matters).  Those that make up more than about a thousandth of everything (where that is not known, those of 2^-6 and more)
+// are formed to about 1e-9 of themselves, the others to fp32: their errors are as often up as down, and 2^-34 of everything at most.  The difference m - x is kept in two parts, and so is 1 / T.  Tokens more than 39 powers of two
 // below the top weigh less than a unit, and nothing.
 #include <cooperative_groups.h>
 
@@ -37,7 +37,7 @@ constexpr int SA_HELD = 32 << 10;       // bytes of a row that a CTA holds in sh
 constexpr float SA_PER_NAT = 32.f;
 constexpr int SA_SORT = 1024;           // members of a bin that are sorted
 constexpr int SA_UNIT = 38;             // weights in units of 2^-38
-constexpr float SA_COARSE = 6.f;        // weights below 2^-6 are formed to fp32
+constexpr float SA_COARSE = 6.f;        // weights below 2^-6 are formed to fp32, where nothing is known of their sum
 constexpr float SA_LAST = 42.f;         // a weight of 2^-42 is none
 typedef unsigned long long u64;
 
@@ -57,7 +57,7 @@ struct SampleShared {
     float table_4[32];                  // the same in units of 4
     u64 sorted[SA_SORT];                // rank 0: members of a bin
     uint32_t count[SA_BINS + 32];       // of the CTA; then, for the bins of this rank's share, of the cluster; 32 for what lies behind all bins
-    u64 sum[2][4][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
+    u64 sum[2][5][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
     float top[SA_WARPS + 1];
     int best[SA_WARPS + 1];
     int members;                        // rank 0: entries of `sorted`
@@ -99,7 +99,7 @@ struct Weigh {
         return down ? (v + (1ull << (down - 1))) >> down : v;
     }
     // To fp32, where x < x_fine (anything elsewhere).  (Two at a time by packed operations, each constant would take two registers.)
-    __device__ __forceinline__ uint32_t coarse(float x) const
+    __device__ __forceinline__ u64 coarse(float x) const
     {
         x = fmaxf(x, x_last);   // (no number, too)
         const float d = m - x;
@@ -115,7 +115,7 @@ struct Weigh {
         q = fmaf(r, q, 0.24022646248340607f);
         q = fmaf(r, q, 0.6931471824645996f);
         q = fmaf(r, q, 1.f);
-        return __float2uint_rn(__int_as_float(__float_as_int(q) + (__float_as_int(n) << 23) + (SA_UNIT << 23)));   // (0x4B400000 << 23 is 0)
+        return __float2ull_rn(__int_as_float(__float_as_int(q) + (__float_as_int(n) << 23) + (SA_UNIT << 23)));   // (0x4B400000 << 23 is 0)
     }
     __device__ __forceinline__ void four(const float4 &x, u64 (&w)[4]) const
     {
@@ -164,7 +164,7 @@ template <> struct Quad<__nv_bfloat16> {
     }
 };
 
-template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, SA_CTAS) sample_kernel(const SampleParams p, int chunk, int places)
+template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, HELD ? 3 : SA_CTAS) sample_kernel(const SampleParams p, int chunk, int places)
 {
     extern __shared__ __align__(16) unsigned char sa_smem[];
     SampleShared &sh = *reinterpret_cast<SampleShared *>(sa_smem);
@@ -311,15 +311,15 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
     const bool by_k = k > 0, by_p = top_p < 1.f;
     const double per = fmin(1.4426950408889634 / (double)T_row, 1e30);
     const float per_hi = (float)per, per_lo = (float)(per - (double)per_hi), d_last = SA_LAST / per_hi;
-    // coarse weights are of logits that are below 2^-6 whatever the roundings here; where logits lie so far apart that x_last cannot be
-    // told from m, or weights fall so slowly that differences overflow, all are weighed finely
-    const Weigh weigh{m, per_hi, per_lo, m - SA_COARSE * 1.001f / per_hi - fabsf(m) * 2.4e-7f, m - d_last,
+    // where logits lie so far apart that x_last cannot be told from m, or weights fall so slowly that differences overflow, all are weighed
+    // finely
+    Weigh weigh{m, per_hi, per_lo, m - SA_COARSE / per_hi, m - d_last,
                       !(fabsf(m) * 2.4e-7f < 0.1f * d_last && fabsf(m) + d_last < 1e37f), sh.table, sh.table_4};
     const float to_bin = (float)fmin((double)SA_PER_NAT / (double)T_row, 1e30);
     auto place_of = [&](float x) { return (m - x) * to_bin; };   // its whole part is the bin; it falls as x rises (no number: in no bin)
 
     int turn = 0;
-    // sums of up to four numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
+    // sums of up to five numbers over the cluster; before: of the first one, of the ranks and warps in front of this warp
     auto cluster_sum = [&](auto &a, auto &all, u64 *before) {
         constexpr int N = (int)(sizeof(a) / sizeof(u64));
 #pragma unroll
@@ -428,26 +428,31 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
             if (have <= SA_SORT) {
                 if (rank == 0) {
                     sort_list(have);
-                    // the first member up to which it is enough, by one warp, 32 members at a time
-                    if (warp == 0) {
-                        u64 sum = 0;
-                        bool found = false;
-                        for (int i = 0; i < have && !found; i += 32) {
-                            const bool there = i + lane < have;
-                            const u64 own_key = sh.sorted[min(i + lane, have - 1)];
-                            u64 upto = there && weights ? weigh.fine(logit_of(own_key)) : 0;
+                    // the first member up to which it is enough: four neighbouring ones per thread, and the sums in front of them
+                    u64 own_w[4], upto = 0;
 #pragma unroll
-                            for (int off = 1; off < 32; off <<= 1) {
-                                const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
-                                if (lane >= off) upto += up;
-                            }
-                            const unsigned yes = __ballot_sync(0xffffffffu, there && enough((uint32_t)(i + lane + 1), sum + upto));
-                            const int at = yes ? __ffs(yes) - 1 : min(31, have - 1 - i);
-                            const u64 k_at = __shfl_sync(0xffffffffu, own_key, at);
-                            found = yes != 0;
-                            if (lane == 0) sh.cut_key = k_at;
-                            sum += __shfl_sync(0xffffffffu, upto, 31);
-                        }
+                    for (int j = 0; j < 4; ++j) {
+                        own_w[j] = weights && tid * 4 + j < have ? weigh.fine(logit_of(sh.sorted[tid * 4 + j])) : 0;
+                        upto += own_w[j];
+                    }
+                    u64 sum = upto;
+#pragma unroll
+                    for (int off = 1; off < 32; off <<= 1) {
+                        const u64 up = __shfl_up_sync(0xffffffffu, upto, off);
+                        if (lane >= off) upto += up;
+                    }
+                    u64 *parts = sh.sum[turn][0];   // (this rank alone; the next sum of the cluster lies behind a barrier)
+                    if (lane == 31) parts[warp] = upto;
+                    if (tid == 0) sh.cut_key = have ? sh.sorted[have - 1] : ~0ull;
+                    __syncthreads();
+                    sum = upto - sum;
+                    for (int i = 0; i < warp; ++i) sum += parts[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int i = tid * 4 + j;
+                        const bool was = i > 0 && enough((uint32_t)i, sum);
+                        sum += own_w[j];
+                        if (i < have && !was && enough((uint32_t)(i + 1), sum)) sh.cut_key = sh.sorted[i];
                     }
                 }
                 cluster.sync();
@@ -615,6 +620,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
             }
             float estimate = 0.f;   // of everything
             for (int i = 0; i < SA_WARPS; ++i) estimate += sh.scan_a[i];
+            // finely weighed: what makes up more than about a thousandth of everything
+            weigh.x_fine = m - fminf(fmaxf((float)(SA_UNIT + 10) - log2f(estimate), 0.f), SA_LAST) / per_hi;
             // the first bin in (from, to) that has members of the prefix and up to whose end about `goal` has gathered; else the last, or -1
             auto search = [&](int from, int to, float goal) {
                 __syncthreads();
@@ -641,7 +648,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
             u64 up = 0, z = 0;
             while (bin >= 0) {   // ends: the bins between low and high get fewer
                 // the weights up to the bin in front of this one, in that one, in this one and in the next; of all of the prefix
-                u64 a[4] = {0, 0, 0, 0}, all[4], z_own[1] = {0}, z_all[1], keep[3] = {0, 0, 0};
+                u64 a[5] = {0, 0, 0, 0, 0}, all[5], keep[3] = {0, 0, 0};
                 const float to = (float)(bin - 1), this_one = (float)bin, next = (float)(bin + 1), behind = (float)(bin + 2);
                 each(from_place, to_place, [&](const float4 &v, int i) {
                     u64 w4[4];
@@ -650,7 +657,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                     for (int j = 0; j < 4; ++j) {
                         const float x = (&v.x)[j], b = place_of(x);
                         if (by_k && !inside(b, x, i + j)) continue;
-                        z_own[0] += w4[j];
+                        a[4] += w4[j];
                         if (b < to) {
                             a[0] += w4[j];
                             if (least && w4[j] >= least) keep[0] += w4[j];
@@ -670,8 +677,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, S
                 });
                 if (!least) keep[0] = a[0];
                 cluster_sum(a, all, nullptr);
-                cluster_sum(z_own, z_all, nullptr);
-                z = z_all[0];
+                z = all[4];
                 const double goal = (double)top_p * (double)z;
                 const u64 to1 = all[0] + all[1], to2 = to1 + all[2], to3 = to2 + all[3];
                 if (all[0] > 0 && (double)all[0] >= goal) high = bin - 1;             // it ends further in front
