@@ -55,12 +55,12 @@ __constant__ u64 powers[32] = {
 struct SampleShared {
     u64 table[32];                      // `powers`
     float table_4[32];                  // the same in units of 4
-    u64 sorted[SA_SORT];                // rank 0: members of a bin
+    u64 sorted[SA_SORT];                // members of a bin; of rank 0, those of all ranks
     uint32_t count[SA_BINS + 32];       // of the CTA; then, for the bins of this rank's share, of the cluster; 32 for what lies behind all bins
     u64 sum[2][5][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
     float top[SA_WARPS + 1];
     int best[SA_WARPS + 1];
-    int members;                        // rank 0: entries of `sorted`
+    int members;                        // entries of `sorted`, of this rank alone
     u64 cut_key;                        // rank 0: where a prefix ends inside a bin
     uint32_t scan_n[SA_WARPS];
     float scan_a[SA_WARPS];
@@ -394,12 +394,28 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
             for (int i = 0; i < warp; ++i) cb += sh.scan_n[i];
         }
         auto in_bin = [&](float b, int bin) { return b >= (float)bin && b < (float)(bin + 1); };
-        // the members of a bin, those of the prefix so far, to rank 0's list
+        // the members of a bin, those of the prefix so far, to this rank's list
+        auto keep_key = [&](float x, int place) {
+            const int at = atomicAdd(&sh.members, 1);
+            if (at < SA_SORT) sh.sorted[at] = key_of(x, index_at(place));
+        };
         auto gather = [&](float b, float x, int place, int bin) {
-            if (in_bin(b, bin) && inside(b, x, place)) {
-                const int at = atomicAdd(cluster.map_shared_rank(&sh.members, 0), 1);
-                if (at < SA_SORT) cluster.map_shared_rank(sh.sorted, 0)[at] = key_of(x, index_at(place));
+            if (in_bin(b, bin) && inside(b, x, place)) keep_key(x, place);
+        };
+        // behind a barrier of the cluster: all ranks' lists to rank 0's; how many members there are (more than SA_SORT: nothing is moved)
+        auto collect = [&]() {
+            int in_front = 0, total = 0;
+            for (int r = 0; r < ranks; ++r) {
+                const int c = *cluster.map_shared_rank(&sh.members, r);
+                if (r < rank) in_front += c;
+                total += c;
             }
+            if (rank != 0 && total <= SA_SORT) {
+                u64 *list = cluster.map_shared_rank(sh.sorted, 0);
+                for (int i = tid; i < sh.members; i += SA_THREADS) list[in_front + i] = sh.sorted[i];
+            }
+            cluster.sync();
+            return total;
         };
         // by rank 0: the list in order, by exchanges at distances that are powers of two; where `have` are fewer than such a power, `none` behind
         auto sort_list = [&](int have) {
@@ -422,8 +438,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
         };
         // The smallest key of the bin's members in the list up to which `enough` holds of the (count, weight) of those with keys up to it;
         // where they were too many for the list, found bit by bit, each with a pass over the row.  After a barrier of the cluster.
-        auto end_in_list = [&](int bin, bool weights, auto enough) {
-            const int have = *cluster.map_shared_rank(&sh.members, 0);
+        auto end_in_list = [&](int bin, int have, bool weights, auto enough) {
             u64 key = ~0ull;
             if (have <= SA_SORT) {
                 if (rank == 0) {
@@ -482,8 +497,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
         };
         auto empty_list = [&]() {
             cluster.sync();   // (everybody has read it)
-            if (rank == 0 && tid == 0) sh.members = 0;
-            cluster.sync();
+            if (tid == 0) sh.members = 0;
+            __syncthreads();
         };
 
         if (by_k) {   // the bin in which the k-th token lies, and its key
@@ -504,14 +519,12 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                 each_short(from_place, to_place, [&](const float4 &v, int i) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (place_of((&v.x)[j]) < (float)(bin + 1)) {
-                            const int at = atomicAdd(cluster.map_shared_rank(&sh.members, 0), 1);
-                            cluster.map_shared_rank(sh.sorted, 0)[at] = key_of((&v.x)[j], index_at(i + j));
-                        }
+                        if (place_of((&v.x)[j]) < (float)(bin + 1)) keep_key((&v.x)[j], i + j);
                 });
                 cluster.sync();
+                const int have = collect();
                 if (rank != 0) return;   // (nobody reads its shared memory any more)
-                sort_list(sh.members);
+                sort_list(have);
                 // weights' sums in falling order, by one warp; how many are kept of the first k
                 int kept_n = k;
                 if (warp == 0) {
@@ -588,7 +601,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                     for (int j = 0; j < 4; ++j) gather(place_of((&v.x)[j]), (&v.x)[j], i + j, bin);
                 });
                 cluster.sync();
-                const u64 key = end_in_list(bin, false, [&](uint32_t cc, u64) { return cc >= wanted; });
+                const int have = collect();
+                const u64 key = end_in_list(bin, have, false, [&](uint32_t cc, u64) { return cc >= wanted; });
                 empty_list();
                 cut_bin = bin;
                 cut_key = key;
@@ -714,8 +728,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
             }
             if (found) {
                 const double goal = (double)top_p * (double)z;
-                const u64 key = end_in_list(bin, true, [&](uint32_t, u64 ww) { return (double)(up + ww) >= goal; });
-                const int have = *cluster.map_shared_rank(&sh.members, 0);
+                const int have = collect();
+                const u64 key = end_in_list(bin, have, true, [&](uint32_t, u64 ww) { return (double)(up + ww) >= goal; });
                 cut_bin = bin;
                 cut_key = key;
                 summed = have <= SA_SORT;
