@@ -39,21 +39,33 @@ struct Choice {
     AttnLayout layout;
 };
 
-// The kernel for a shape, its grid, and the places in the workspace; false: more units than a grid has CTAs.
+// Grid of a kernel with the given tiles, and whether units are split; false: more units than a grid has CTAs.
+bool place(const gdn_attn_shape_t &s, const AttnTiling &t, Choice &c)
+{
+    const long long rows = (long long)s.max_rows * (s.h_q / s.h_kv);
+    c.tiling = t;
+    c.m_tiles = (int)((rows + t.M - 1) / t.M);
+    const long long units = (long long)s.n_seq * s.h_kv * c.m_tiles, tiles = ((long long)s.max_len + t.TN - 1) / t.TN;
+    if (units > 0x7fffffffLL) return false;
+    const long long resident = (long long)t.ctas * AT_SMS;
+    // a chunk of a prompt with more units than two for every CTA goes without: its units see ever more tokens, and the longest begin first
+    c.split = tiles > 1 && !(c.m_tiles > 1 && units >= 2 * resident);
+    c.grid = (int)(!c.split ? units : units * tiles < resident ? units * tiles : resident);
+    return true;
+}
+
+// The kernel for a shape, its grid, and the places in the workspace.
 bool choose(const gdn_attn_shape_t &s, Choice &c)
 {
     const long long rows = (long long)s.max_rows * (s.h_q / s.h_kv);
     // up to 64 rows per key/value head the keys and values decide, and one tile of rows reads them once; above, the products do.
     // (The kernel of the latter takes maxima of unscaled scores: a scale that turns or hides their order is the other's.)
     c.kernel = !(s.dtype == GDN_BF16 && (s.d == 64 || s.d == 128)) ? Choice::GENERAL : rows <= 64 || !(s.scale > 0.f) ? Choice::ROWS : Choice::SM100;
-    c.tiling = c.kernel == Choice::GENERAL ? attn_general_tiling(s.dtype == GDN_BF16, s.d) : c.kernel == Choice::ROWS ? attn_rows_tiling((int)rows, s.d) : attn_sm100_tiling();
-    c.m_tiles = (int)((rows + c.tiling.M - 1) / c.tiling.M);
-    const long long units = (long long)s.n_seq * s.h_kv * c.m_tiles, tiles = ((long long)s.max_len + c.tiling.TN - 1) / c.tiling.TN;
-    if (units > 0x7fffffffLL) return false;
-    const long long resident = (long long)c.tiling.ctas * AT_SMS;
-    // a chunk of a prompt with more units than two for every CTA goes without: its units see ever more tokens, and the longest begin first
-    c.split = tiles > 1 && !(c.m_tiles > 1 && units >= 2 * resident);
-    c.grid = (int)(!c.split ? units : units * tiles < resident ? units * tiles : resident);
+    const AttnTiling by_rows = attn_rows_tiling(rows < 64 ? (int)rows : 64, s.d);
+    Choice other;   // (one workspace serves all scales)
+    if (!place(s, c.kernel == Choice::GENERAL ? attn_general_tiling(s.dtype == GDN_BF16, s.d) : c.kernel == Choice::ROWS ? by_rows : attn_sm100_tiling(), c) ||
+        !place(s, by_rows, other))
+        return false;
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
@@ -64,9 +76,15 @@ bool choose(const gdn_attn_shape_t &s, Choice &c)
     const bool masks = s.max_rows > AT_SMALL_ROWS && s.max_rows <= GDN_MAX_TREE_NODES;
     c.layout.mask = take(masks ? sizeof(uint32_t) * (size_t)s.total_rows * ((s.max_rows + 31) / 32) : 0);
     c.layout.tree_ok = take(masks ? sizeof(int32_t) * (size_t)s.n_seq : 0);
-    const size_t parts = c.split ? 2 * (size_t)c.grid * c.tiling.M : 0;
-    c.layout.part_o = take(parts * s.d * sizeof(float));
-    c.layout.part_ml = take(parts * 2 * sizeof(float));
+    auto parts = [](const Choice &x) { return x.split ? 2 * (size_t)x.grid * x.tiling.M : 0; };
+    size_t most = parts(c);
+    if (c.kernel != Choice::GENERAL && rows > 64) {
+        Choice tall;
+        if (!place(s, attn_sm100_tiling(), tall)) return false;
+        most = parts(tall) > parts(other) ? parts(tall) : parts(other);
+    }
+    c.layout.part_o = take(most * s.d * sizeof(float));
+    c.layout.part_ml = take(most * 2 * sizeof(float));
     c.layout.total = off ? off : 256;
     return true;
 }

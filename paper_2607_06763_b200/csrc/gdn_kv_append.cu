@@ -53,14 +53,16 @@ template <> struct Piece<__nv_bfloat16> {
     }
 };
 
-// The last of the ascending offsets[0 .. n] that is at most x (by a whole warp; offsets[0] = 0 <= x < offsets[n]).
+// The last of the ascending offsets[0 .. n - 1] that is at most x, -1 where the first is not (by a whole warp).
 __device__ __forceinline__ int warp_search(const int32_t *offsets, int n, int x, int lane)
 {
-    int lo = 0, hi = n;   // offsets[lo] <= x < offsets[hi]
+    int lo = 0, hi = n;
+    if (offsets[0] > x) return -1;
     while (hi - lo > 1) {
         const int step = (hi - lo + 31) / 32, i = lo + lane * step;
         const unsigned le = __ballot_sync(0xffffffffu, i < hi && offsets[i] <= x);
-        const int top = 31 - __clz((int)le);   // (lane 0 is among them)
+        if (le == 0) return -1;   // (offsets that do not ascend)
+        const int top = 31 - __clz((int)le);
         lo += top * step;
         hi = min(lo + step, hi);
     }
@@ -104,13 +106,19 @@ template <typename T, bool VEC> __global__ void __launch_bounds__(KA_WARPS * 32)
     const int index = (int)(w / parts), part = (int)(w % parts);
     const int32_t *offsets = p.path ? p.path_offsets : a.row_offsets;
     const int count = offsets[a.n_seq];
-    if (index >= count || (!p.path && index >= a.total_rows)) return;
+    const int bad_offsets = p.path ? GDN_ERR_PATH : GDN_ERR_TREE;
+    if (w == 0 && count > a.total_rows && lane == 0) report_status(a.status_dev, bad_offsets);
+    if (index >= count || index >= a.total_rows) return;
     const int b = warp_search(offsets, a.n_seq, index, lane);
-    const int t = index - offsets[b];
     AttnSeq s;
+    if (b < 0) {
+        if (lane == 0) report_status(a.status_dev, bad_offsets);
+        return;
+    }
+    const int t = index - offsets[b];
     if (!attn_seq(a, b, s, true)) return;
     if (t < 0 || (!p.path && t >= s.rows)) {
-        if (lane == 0) report_status(a.status_dev, p.path ? GDN_ERR_PATH : GDN_ERR_TREE);
+        if (lane == 0) report_status(a.status_dev, bad_offsets);
         return;
     }
     int row = s.row0 + t, depth = t;   // (the length of what is written counts into max_len with all rows of the call)

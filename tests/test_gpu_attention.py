@@ -28,7 +28,7 @@ class Call:
         import paper_2607_06763_b200 as gdn
         rng = np.random.default_rng(seed)
         self.gdn, self.lens, self.rows, self.d, self.dtype, self.decode = gdn, list(lens), list(rows), d, dtype, decode
-        self.h_q, self.h_kv = h_q, h_kv
+        self.h_q, self.h_kv, self.scale = h_q, h_kv, d ** -0.5
         held = self.lens if decode else [a + b for a, b in zip(lens, rows)]
         self.held = held
         self.cache = at.Cache(rng, [n + slack for n in held], h_kv, d, page, dtype, layout, strides=strides)
@@ -81,7 +81,7 @@ class Call:
         for b in range(len(self.lens)) if only is None else only:
             k, v = self.cache.read(b, self.held[b])
             rows = slice(int(self.offsets[b]), int(self.offsets[b + 1]))
-            o, a, big = at.attend(self.q64[rows], k, v, self.see(b), self.d ** -0.5)
+            o, a, big = at.attend(self.q64[rows], k, v, self.see(b), self.scale)
             bound = at.allowed(o, a, big, self.dtype, self.d, self.held[b])
             assert np.array_equal(np.isfinite(got[rows]), np.isfinite(o)), f"{what}: finite in other places, sequence {b}"
             fine = np.isfinite(o)
@@ -138,6 +138,38 @@ def test_chunks_of_a_prompt(cuda_device, rows, h_q, h_kv, d, dtype):
 @pytest.mark.parametrize("h_q,h_kv,d", [(8, 2, 128), (8, 1, 64)])
 def test_trees_behind_long_caches(cuda_device, lens, rows, h_q, h_kv, d):
     Call(6, lens, rows, h_q, h_kv, d, page=64, slack=100).verify()
+
+
+@pytest.mark.parametrize("page,layout", [(1, "token"), (7, "head"), (8, "token"), (24, "head"), (100, "token"), (256, "head")])
+@pytest.mark.parametrize("h_q,h_kv,d", [(8, 1, 128), (8, 1, 64), (2, 2, 128)])
+def test_tree_pages(cuda_device, page, layout, h_q, h_kv, d):
+    """Units of more than 64 rows by tensor copies (pages that a power of two from 8 on divides) and by rows."""
+    Call(15, [300, 0, 65], [60, 64, 17], h_q, h_kv, d, page=page, layout=layout, strides=8, spare_rows=1).verify()
+    Call(16, [300, 40], [90, 130], h_q, h_kv, d, page=page, layout=layout, chain=True).verify()
+
+
+@pytest.mark.parametrize("decode", [True, False])
+@pytest.mark.parametrize("h_q,h_kv,d", [(80, 1, 64), (160, 1, 128), (300, 1, 64)])
+def test_many_heads_share_one(cuda_device, decode, h_q, h_kv, d):
+    lens = [0, 1, 127, 700]
+    Call(17, lens, [1] * 4 if decode else [3, 1, 0, 2], h_q, h_kv, d, decode=decode).verify()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1e-30])
+@pytest.mark.parametrize("rows", [[5, 2], [70, 30]], ids=str)
+def test_scales_that_hide_or_turn_the_order(cuda_device, scale, rows):
+    c = Call(18, [90, 300], rows, 8, 2, 64)
+    c.shape.scale = c.scale = scale
+    c.verify()
+
+
+def test_many_sequences_of_all_lengths(cuda_device):
+    """More units than runs, of a tile to a hundred: runs over many units and units over many runs."""
+    rng = np.random.default_rng(19)
+    lens = [int(x) for x in np.exp(rng.uniform(0, np.log(9000), 60))]
+    Call(20, lens, [1] * 60, 4, 2, 64, decode=True, page=64).verify()
+    Call(21, lens, [int(x) for x in rng.integers(0, 20, 60)], 8, 2, 64, page=32).verify()
+    Call(22, lens[:30], [int(x) for x in rng.integers(20, 64, 30)], 8, 2, 128, page=32).verify()
 
 
 @pytest.mark.parametrize("h_q,h_kv,d,dtype", [(4, 4, 64, "bf16"), (8, 1, 128, "bf16"), (4, 2, 64, "f32")])
@@ -430,6 +462,16 @@ def test_append_in_place_and_faults(cuda_device):
     c.page_table[2, 1] = 1 << 20   # where rows 30, 31 of the last sequence would go
     out2 = torch.zeros_like(q)
     assert run(c, q, out2) == -12 and np.isnan(c.read(0, 112)[0]).sum() < 112 * h_kv * d
+    for wrong in ([2, 4, 84, 86], [0, 4, 84, 1 << 20], [0, 84, 4, 86], [-5, 4, 84, 86], [0, 4, 84, 87]):
+        c = cache()
+        shape = gdn.GdnAttnShape.from_cache(c.k, c.page_table, h_q, N, max(rows), max_len=112)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out3 = torch.zeros_like(q)
+        assert gdn.gdn_kv_append(shape, q, k, v, rope, 128, 64, 0, None, _ints(wrong), _ints(lens), c.page_table, out3, c.k, c.v, status) == 0
+        assert gdn.gdn_kv_commit(shape, k, v, rope, 128, 64, 0, None, _ints(offsets), _ints([0] * 200), _ints(wrong), _ints(lens), c.page_table,
+                                 c.k, c.v, status) == 0
+        torch.cuda.synchronize()
+        assert int(status.item()) in (-7, -9), wrong
     bad = [p.copy() for p in parents]
     bad[1][40] = 50
     c = cache()
