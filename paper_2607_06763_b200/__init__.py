@@ -1,7 +1,8 @@
 """B200-native GDN tree verification and commit (Section 3.4 of "Trees from Marginals").
 
 ``gdn_tree_verify`` and ``gdn_tree_commit`` are thin bindings over the C-ABI CUDA library built from ``csrc/``;
-``synth`` holds the seeded synthetic workload generators.  There is no CPU fallback: every call raises if the CUDA
+``gdn_kv_append``, ``gdn_kv_commit``, ``gdn_attn_decode``, ``gdn_attn_tree_verify`` and ``gdn_sample``
+serve the full-attention layers and the output layer of the same model; ``synth`` holds the seeded synthetic workload generators.  There is no CPU fallback: every call raises if the CUDA
 library has not been built.
 """
 from . import synth  # noqa: F401

@@ -10,9 +10,10 @@
 // weights up to 256 are as exact in bf16, and O is multiplied only where a row's maximum has risen by more.
 //
 // Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, which warp 11 looks at where
-// not all rows see them, warp 10 the products.  Two or more stages of keys and of values, each with its own barriers.  Pages whose size is a multiple of 8 come by tensor copies, a page
-// or a part of one each, straight into the swizzled layout of the products' operands; others by cp.async, row by row: one warp needs
-// 3300 clocks to issue a tile that way, the products of two streams 2048.
+// not all rows see them, warp 10 the products.  Two or more stages of keys and of values, each with its own barriers.  Pages whose size
+// is a multiple of 8 come by tensor copies, a page or a part of one each, straight into the swizzled layout of the products' operands;
+// others by cp.async, row by row: one warp needs 3300 clocks to issue a tile that way, the products of two streams 2048 (trees of 32
+// sequences: 335 us with pages of 7 tokens, 213 with pages of 16).
 // A row's 128 scores stay in its thread's registers (the warps of the rows take over what the others leave).
 // Every wait is bounded; one that expires raises a flag that ends the others.
 #include "gdn_attn.cuh"
@@ -26,13 +27,14 @@ constexpr int AS_M = 256, AS_TN = 128, AS_MOST = 4;
 constexpr float AS_SLACK = 8.f;   // a maximum may rise by this many powers of two before the sums follow
 
 template <int D> __host__ __device__ constexpr int as_tile_bytes() { return AS_TN * D * 2; }
-// Tiles of keys, and of values, on their way or at work: what shared memory holds beside the queries.  (With two of values, a tile's copy
-// of small pages, 4000 clocks, began too late: trees of 32 sequences 250 us instead of the present figure in the table.)
+// Tiles of keys, and of values, on their way or at work: what shared memory holds beside the queries.  (A tile's copy of
+// pages of 24 tokens takes 4000 clocks, the work on a tile 3300: with two tiles of values, and one of them on its way at a time, trees of 32
+// sequences took 250 us, with three 225.)
 template <int D> __host__ __device__ constexpr int as_k_stages() { return D == 128 ? 2 : 4; }
 template <int D> __host__ __device__ constexpr int as_v_stages() { return D == 128 ? 3 : 4; }
 template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t)as_tile_bytes<D>() * (2 + as_k_stages<D>() + as_v_stages<D>()) + 1024; }
 
-struct SplitShared {
+struct UnitShared {
     unsigned long long anc[AT_SMALL_ROWS];
     int anc_up[AT_SMALL_ROWS];
     unsigned long long q_full, k_full[AS_MOST], v_full[AS_MOST], v_landed[AS_MOST], k_empty[AS_MOST], v_empty[AS_MOST], s_full[2], p_full[2][2], o_full[2];   // p_full: [half of the tile][stream]
@@ -54,15 +56,6 @@ __device__ __forceinline__ void umma_bf16_ts_into(uint32_t d_tmem, uint32_t a_tm
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
-#define GDN_TMEM_ST32(taddr, r)                                                                              \
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "                                             \
-                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"                                  \
-                 "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"                         \
-                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),       \
-                   "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), \
-                   "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),           \
-                   "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])                        \
-                 : "memory")
 #define GDN_TMEM_ST16(taddr, r)                                                                              \
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"    \
                  ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),       \
@@ -169,7 +162,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 {
     constexpr int TILE = as_tile_bytes<D>(), KS = D / 16, PIECES = D / 8, K_STAGES = as_k_stages<D>(), V_STAGES = as_v_stages<D>();
     extern __shared__ __align__(16) unsigned char as_raw[];
-    __shared__ SplitShared sh;
+    __shared__ UnitShared sh;
     unsigned char *const data = as_raw + ((1024u - (smem_u32(as_raw) & 1023u)) & 1023u);   // swizzled tiles begin on 1024 bytes
     const uint32_t q_s = smem_u32(data), k_s = q_s + 2 * TILE, v_s = k_s + K_STAGES * TILE;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cta = (int)blockIdx.x;
