@@ -125,7 +125,18 @@ __device__ __forceinline__ long long warp_sum(long long x)
 // What all runs together hold, and what of it lies in the sequences of this lane and in front of sequence `before_b`, by a whole warp.
 struct AttnTotal {
     long long total, mine, before;
-    int over;   // tiles that a unit counts for beyond its own
+    int over;        // tiles that a unit counts for beyond its own
+    long long per;   // small calls: tiles of a run (as many as the longest would have if all were alike, so that fewer runs lie across two units); else 0
+    __device__ __forceinline__ long long runs(const AttnParams &p) const
+    {
+        return per ? times_over(total + per - 1, 1, per) : total < p.n_ctas ? total : p.n_ctas;
+    }
+    __device__ __forceinline__ long long begin(long long run, long long runs) const { return per ? min(run * per, total) : times_over(total, run, runs); }
+    // of a place of the total, the last run that begins at it or in front of it
+    __device__ __forceinline__ int run_of(long long place, long long runs) const
+    {
+        return (int)(per ? times_over(place, 1, per) : times_over((place + 1) * runs - 1, 1, total));
+    }
 };
 template <bool BEFORE> __device__ __forceinline__ AttnTotal attn_total(const AttnParams &p, int M, int TN, int before_b, bool report)
 {
@@ -144,8 +155,9 @@ template <bool BEFORE> __device__ __forceinline__ AttnTotal attn_total(const Att
     }
     const long long all_tiles = warp_sum(tiles), all_units = __reduce_add_sync(0xffffffffu, (uint32_t)units);
     AttnTotal r;
-    r.over = all_tiles >= 4ll * p.n_ctas ? p.over : 0;
+    r.over = all_tiles >= 4ll * p.n_ctas ? p.over : 0;   // (p.over > 0)
     r.total = all_tiles + all_units * r.over;
+    r.per = r.over ? 0 : times_over(all_tiles + p.n_ctas - 1, 1, p.n_ctas);
     r.mine = tiles + units * r.over;
     r.before = BEFORE ? warp_sum(tiles_before + units_before * r.over) : 0;
     return r;
@@ -168,13 +180,13 @@ struct AttnWalk {
         const int lane = threadIdx.x & 31;
         const int per = (p.n_seq + 31) / 32, b0 = min(lane * per, p.n_seq), b1 = min(b0 + per, p.n_seq);
         const AttnTotal sum = attn_total<false>(p, M, TN, 0, cta == 0 && threadIdx.x < 32);
-        const long long mine = sum.mine, upto = warp_scan(mine, lane), total = sum.total;
+        const long long mine = sum.mine, upto = warp_scan(mine, lane);
         over = sum.over;
-        const long long runs = total < p.n_ctas ? total : p.n_ctas;
+        const long long runs = sum.runs(p);
         at = end = 0;
         if (cta >= runs) return;
-        at = times_over(total, cta, runs);
-        end = times_over(total, cta + 1, runs);
+        at = sum.begin(cta, runs);
+        end = sum.begin(cta + 1, runs);
         // the lane whose sequences hold tile `at` looks for it among them
         const unsigned holds = __ballot_sync(0xffffffffu, upto > at);
         const int owner = __ffs(holds) - 1;

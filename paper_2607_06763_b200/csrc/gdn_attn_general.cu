@@ -278,11 +278,6 @@ __global__ void __launch_bounds__(AM_THREADS) attn_mask_kernel(const AttnParams 
     }
 }
 
-__device__ __forceinline__ int run_of(long long tile, long long runs, long long total)
-{
-    return (int)times_over((tile + 1) * runs - 1, 1, total);
-}
-
 // The parts of a split unit, in the order of their tiles, to its rows: o = sum_p 2^(m_p - m) o_p / sum_p 2^(m_p - m) l_p.
 // A thread has four components of a row; the threads of a CTA read neighbouring pieces of each part, which lie [M][d / 4] or, where a
 // thread of the kernel in front has a row (columns_first), [d / 4][M].  A unit that one run held is left alone.
@@ -316,9 +311,8 @@ template <typename T> __global__ void __launch_bounds__(AJ_THREADS) attn_join_ke
     }
     const int tiles = attn_tiles(s, TN), m_tiles = (s.rows * p.group + M - 1) / M;
     const long long first = sum.before + (long long)(head * m_tiles + m_tile) * (tiles + sum.over) + sum.over, last = first + tiles - 1;
-    const long long total = sum.total, runs = total < p.n_ctas ? total : p.n_ctas;
-    // run c begins at total * c / runs; a tile's is the last that begins at it or in front of it
-    const int c0 = run_of(first, runs, total), c1 = run_of(last, runs, total);
+    const long long runs = sum.runs(p);
+    const int c0 = sum.run_of(first, runs), c1 = sum.run_of(last, runs);
     wait_for_previous_kernel();
     if (bad || c0 == c1) return;
 
