@@ -8,13 +8,13 @@
 // A row belongs to the CTAs of a cluster (one to eight).  They go over it two to four times: from shared memory where a CTA's part is
 // small (few rows: what counts is the time of a pass), else from where the first reading left it, L2 (many rows: what counts is how
 // many CTAs an SM holds; the rows at work at one time are some 100 MB at most).  Nothing is sorted but the
-// members of one bin: (m - x) / T in units of 1/32 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
+// members of one bin: (m - x) / T in units of 1/64 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
 // The first k end in a bin that the counts tell.  Where the p end the counts nearly tell: a count times the weight at the bin's middle
 // is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, in it and
 // its neighbours, and altogether, and sees whether it is one of the three (else the estimate starts again from these sums).  Only that bin's members (some hundreds
 // of 131071) are put in order; a bin with more members than fit (many equal logits) is bisected instead.  What the pass summed up
 // to the bin, warp by warp, also says where the token lies.
-// The first k of a row, k up to a thousand, are put in order at once, and the row is done with.
+// The first k of a row, k up to two thousand, are put in order at once, and the row is done with.
 //
 // A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-38 (no order
 // of additions matters).  Those that make up more than about a thousandth of everything (where that is not known, those of 2^-6 and more)
@@ -32,10 +32,10 @@ namespace gdn {
 namespace {
 
 constexpr int SA_THREADS = 256, SA_WARPS = SA_THREADS / 32, SA_CTAS = 4;
-constexpr int SA_BINS = 1024, SA_OWN = SA_BINS / SA_THREADS;   // bins, of a thread
+constexpr int SA_BINS = 2048, SA_OWN = SA_BINS / SA_THREADS;   // bins, of a thread
 constexpr int SA_HELD = 32 << 10;       // bytes of a row that a CTA holds in shared memory
-constexpr float SA_PER_NAT = 32.f;
-constexpr int SA_SORT = 1024;           // members of a bin that are sorted
+constexpr float SA_PER_NAT = 64.f;
+constexpr int SA_SORT = 2048;           // members of a bin that are sorted; more are bisected, which takes some 40 passes: 0.7 ms for 131071 logits
 constexpr int SA_UNIT = 38;             // weights in units of 2^-38
 constexpr float SA_COARSE = 6.f;        // weights below 2^-6 are formed to fp32, where nothing is known of their sum
 constexpr float SA_LAST = 42.f;         // a weight of 2^-42 is none
@@ -69,6 +69,59 @@ struct SampleShared {
     bool few;                           // tokens down to the end of `bin`
 };
 
+// Weight of the token with logit x in units, to about 1e-9 of itself, whatever its size (see Weigh).  A function of its own, as the other
+// steps that are taken now and then are: inlined wherever they are called they make code that few rows never find in the
+// instruction cache.
+__device__ __noinline__ u64 weigh_finely(float x, float m, float per_hi, float per_lo, const u64 *table, const float *table_4)
+{
+    if (x == m) return 1ull << SA_UNIT;
+    const float d = m - x;
+    if (!(d * per_hi < SA_LAST && d < INFINITY)) return 0;
+    // m - x = d + lo exactly
+    const float back = d - m, lo = (m - (d - back)) + (-x - back);
+    const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
+    const float err = fmaf(lo, per_hi, fmaf(d, per_hi, -t) + d * per_lo);
+    const float t32 = t * 32.f;
+    const float shifted = t32 + 12582912.f;                 // 1.5 * 2^23: rounds to a whole number
+    const int n = __float_as_int(shifted) - 0x4B400000;
+    const float r = -((t32 - (shifted - 12582912.f)) + 32.f * err) * 0.021660849392498290f;   // ln(2) / 32
+    // e^r - 1 of |r| <= 0.011: the terms of its series
+    const float q = r * fmaf(r, fmaf(r, fmaf(r, 0.041666666666666664f, 0.16666666666666666f), 0.5f), 1.f);
+    // (the correction is below 2^38 * 0.011 < 2^32: in units of 4 it fits a 32-bit number)
+    const u64 v = table[n & 31] + (u64)((long long)__float2int_rn(table_4[n & 31] * q) * 4);
+    const int down = n >> 5;
+    return down ? (v + (1ull << (down - 1))) >> down : v;
+}
+
+// The same without the unit's rounding, of one token that weighs something.
+__device__ __noinline__ double weigh_exactly(float x, float m, float per_hi, float per_lo)
+{
+    return (x == m ? 1.0 : exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453)) * (double)(1ull << SA_UNIT);
+}
+
+// By a whole CTA: `have` keys in rising order, by exchanges at distances that are powers of two; the greatest number stands behind them
+// up to such a power.
+__device__ __noinline__ void sort_keys(u64 *keys, int have)
+{
+    const int tid = threadIdx.x;
+    int size = 32;
+    while (size < have) size *= 2;
+    for (int i = have + tid; i < size; i += SA_THREADS) keys[i] = ~0ull;
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+        for (int apart = run / 2; apart; apart /= 2) {
+            for (int i = tid; i < size / 2; i += SA_THREADS) {
+                const int a = 2 * i - (i & (apart - 1)), b = a + apart;
+                const u64 ka = keys[a], kb = keys[b];
+                if ((ka > kb) == ((a & run) == 0)) {
+                    keys[a] = kb;
+                    keys[b] = ka;
+                }
+            }
+            __syncthreads();
+        }
+}
+
 // Weights in units of tokens with given logits; per = log2(e) / T in two parts.
 struct Weigh {
     float m, per_hi, per_lo;
@@ -77,27 +130,7 @@ struct Weigh {
     const u64 *table;
     const float *table_4;
 
-    // To about 1e-9, whatever the size.
-    __device__ __forceinline__ u64 fine(float x) const
-    {
-        if (x == m) return 1ull << SA_UNIT;
-        const float d = m - x;
-        if (!(d * per_hi < SA_LAST && d < INFINITY)) return 0;
-        // m - x = d + lo exactly
-        const float back = d - m, lo = (m - (d - back)) + (-x - back);
-        const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
-        const float err = fmaf(lo, per_hi, fmaf(d, per_hi, -t) + d * per_lo);
-        const float t32 = t * 32.f;
-        const float shifted = t32 + 12582912.f;                 // 1.5 * 2^23: rounds to a whole number
-        const int n = __float_as_int(shifted) - 0x4B400000;
-        const float r = -((t32 - (shifted - 12582912.f)) + 32.f * err) * 0.021660849392498290f;   // ln(2) / 32
-        // e^r - 1 of |r| <= 0.011: the terms of its series
-        const float q = r * fmaf(r, fmaf(r, fmaf(r, 0.041666666666666664f, 0.16666666666666666f), 0.5f), 1.f);
-        // (the correction is below 2^38 * 0.011 < 2^32: in units of 4 it fits a 32-bit number)
-        const u64 v = table[n & 31] + (u64)((long long)__float2int_rn(table_4[n & 31] * q) * 4);
-        const int down = n >> 5;
-        return down ? (v + (1ull << (down - 1))) >> down : v;
-    }
+    __device__ __forceinline__ u64 fine(float x) const { return weigh_finely(x, m, per_hi, per_lo, table, table_4); }
     // To fp32, where x < x_fine (anything elsewhere).  (Two at a time by packed operations, each constant would take two registers.)
     __device__ __forceinline__ u64 coarse(float x) const
     {
@@ -132,11 +165,7 @@ struct Weigh {
                 if ((&x.x)[j] > x_fine) w[j] = fine((&x.x)[j]);
         }
     }
-    // Of a token that weighs something, in units, not rounded to one.
-    __device__ double exactly(float x) const
-    {
-        return (x == m ? 1.0 : exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453)) * (double)(1ull << SA_UNIT);
-    }
+    __device__ __forceinline__ double exactly(float x) const { return weigh_exactly(x, m, per_hi, per_lo); }
 };
 
 __device__ __forceinline__ uint32_t ordered(float x)   // as unsigned numbers in the order of x
@@ -417,37 +446,19 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
             cluster.sync();
             return total;
         };
-        // by rank 0: the list in order, by exchanges at distances that are powers of two; where `have` are fewer than such a power, `none` behind
-        auto sort_list = [&](int have) {
-            int size = 32;
-            while (size < have) size *= 2;
-            for (int i = have + tid; i < size; i += SA_THREADS) sh.sorted[i] = ~0ull;
-            __syncthreads();
-            for (int run = 2; run <= size; run *= 2)
-                for (int apart = run / 2; apart; apart /= 2) {
-                    for (int i = tid; i < size / 2; i += SA_THREADS) {
-                        const int a = 2 * i - (i & (apart - 1)), b = a + apart;
-                        const u64 ka = sh.sorted[a], kb = sh.sorted[b];
-                        if ((ka > kb) == ((a & run) == 0)) {
-                            sh.sorted[a] = kb;
-                            sh.sorted[b] = ka;
-                        }
-                    }
-                    __syncthreads();
-                }
-        };
         // The smallest key of the bin's members in the list up to which `enough` holds of the (count, weight) of those with keys up to it;
         // where they were too many for the list, found bit by bit, each with a pass over the row.  After a barrier of the cluster.
         auto end_in_list = [&](int bin, int have, bool weights, auto enough) {
             u64 key = ~0ull;
             if (have <= SA_SORT) {
                 if (rank == 0) {
-                    sort_list(have);
-                    // the first member up to which it is enough: four neighbouring ones per thread, and the sums in front of them
-                    u64 own_w[4], upto = 0;
+                    sort_keys(sh.sorted, have);
+                    // the first member up to which it is enough: some neighbouring ones per thread, and the sums in front of them
+                    constexpr int OWN = SA_SORT / SA_THREADS;
+                    u64 own_w[OWN], upto = 0;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        own_w[j] = weights && tid * 4 + j < have ? weigh.fine(logit_of(sh.sorted[tid * 4 + j])) : 0;
+                    for (int j = 0; j < OWN; ++j) {
+                        own_w[j] = weights && tid * OWN + j < have ? weigh.fine(logit_of(sh.sorted[tid * OWN + j])) : 0;
                         upto += own_w[j];
                     }
                     u64 sum = upto;
@@ -463,8 +474,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                     sum = upto - sum;
                     for (int i = 0; i < warp; ++i) sum += parts[i];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int i = tid * 4 + j;
+                    for (int j = 0; j < OWN; ++j) {
+                        const int i = tid * OWN + j;
                         const bool was = i > 0 && enough((uint32_t)i, sum);
                         sum += own_w[j];
                         if (i < have && !was && enough((uint32_t)(i + 1), sum)) sh.cut_key = sh.sorted[i];
@@ -473,7 +484,13 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                 cluster.sync();
                 key = *cluster.map_shared_rank(&sh.cut_key, 0);
             } else {
+                // (from the ends of the bin, a little further apart than rounding can put them)
                 u64 lo = 0, hi = ~0ull;
+                const float above = m - (float)bin / to_bin, below = m - (float)(bin + 1) / to_bin, more = (fabsf(above) + fabsf(below) + fabsf(m)) * 1e-5f;
+                if (below - more > -3e38f && above + more < 3e38f) {
+                    lo = key_of(above + more, 0);
+                    hi = key_of(below - more, -1);
+                }
                 while (lo < hi) {
                     const u64 mid = lo + (hi - lo) / 2;
                     u64 a[2] = {0, 0}, all[2];
@@ -524,7 +541,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                 cluster.sync();
                 const int have = collect();
                 if (rank != 0) return;   // (nobody reads its shared memory any more)
-                sort_list(have);
+                sort_keys(sh.sorted, have);
                 // weights' sums in falling order, by one warp; how many are kept of the first k
                 int kept_n = k;
                 if (warp == 0) {
@@ -564,7 +581,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                     sh.sorted[i] = key << 32 | key >> 32;
                 }
                 __syncthreads();
-                sort_list(kept_n);
+                sort_keys(sh.sorted, kept_n);
                 if (warp == 0) {
                     auto logit_at = [&](int i) { return logit_of(sh.sorted[i] << 32); };
                     u64 z = 0;
