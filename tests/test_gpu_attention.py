@@ -172,6 +172,24 @@ def test_many_sequences_of_all_lengths(cuda_device):
     Call(22, lens[:30], [int(x) for x in rng.integers(20, 64, 30)], 8, 2, 128, page=32).verify()
 
 
+@pytest.mark.parametrize("chain", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_units_than_two_per_cta(cuda_device, chain, d):
+    """Units that are not split: chunks and trees of many sequences, some without rows, one that is no tree."""
+    rng = np.random.default_rng(24)
+    lens = [int(x) for x in rng.integers(0, 200, 16)]
+    rows = [int(x) for x in rng.integers(0, 90, 16)]
+    rows[3], rows[5] = 0, 100
+    c = Call(25, lens, rows, 32, 8, d, page=16, chain=chain, spare_rows=2)
+    c.verify()
+    if not chain:
+        c.o.fill_(7.0)
+        c.parent[int(c.offsets[5]) + 50] = 60
+        assert c.run() == 0 and c.device_status() == -7
+        c.check(only=[b for b in range(16) if b != 5])
+        assert (c.o[int(c.offsets[5]):int(c.offsets[6])] == 7.0).all()
+
+
 @pytest.mark.parametrize("h_q,h_kv,d,dtype", [(4, 4, 64, "bf16"), (8, 1, 128, "bf16"), (4, 2, 64, "f32")])
 @pytest.mark.parametrize("rows", [[9], [40, 64], [150]], ids=str)
 @pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")], ids=str)
