@@ -265,15 +265,16 @@ __device__ __forceinline__ long long attn_token_offset(const AttnParams &p, int 
 }
 
 // Ancestors of the nodes of a tree of at most 64 nodes, the node itself among them, for all threads of the CTA, by its first warp
-// (two nodes per lane); a and up are [64] each.  False where the tree is none.  Doubling: after k rounds a node knows its next 2^k
-// ancestors.
-__device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSeq &s, unsigned long long *a, int *up, int *good)
+// (two nodes per lane); a and up are [64] each.  False where the tree is none, for all threads alike: the verdict comes with the barrier, for a
+// flag in shared memory could be that of the next unit's tree before the last thread has read it.  Doubling: after k rounds a node knows
+// its next 2^k ancestors.
+__device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSeq &s, unsigned long long *a, int *up)
 {
     const int lane = threadIdx.x;
+    bool bad = false;
     if (lane < 32) {
         int next[2];
         unsigned long long seen[2];
-        bool bad = false;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int i = lane + 32 * h;
@@ -281,7 +282,6 @@ __device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSe
             bad |= next[h] < -1 || next[h] >= i;
         }
         bad = __any_sync(0xffffffffu, bad);
-        if (lane == 0) *good = !bad;
         for (int step = 1; !bad && step < 2 * s.rows; step <<= 1) {   // (the last round only writes)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -300,8 +300,7 @@ __device__ __forceinline__ bool attn_ancestors(const AttnParams &p, const AttnSe
             __syncwarp();
         }
     }
-    __syncthreads();
-    return *good != 0;
+    return !__syncthreads_or(bad);
 }
 
 // Whether row node i sees node j of its sequence's rows (i, j < rows).

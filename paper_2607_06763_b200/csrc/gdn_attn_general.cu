@@ -41,7 +41,7 @@ template <typename T, int DD> __global__ void __launch_bounds__(AG_THREADS, 3) a
 {
     extern __shared__ __align__(16) unsigned char ag_smem_base[];
     __shared__ unsigned long long anc[AT_SMALL_ROWS];
-    __shared__ int anc_up[AT_SMALL_ROWS], tree_good;
+    __shared__ int anc_up[AT_SMALL_ROWS];
     const int d = DD ? DD : p.d, pitch = ag_pitch<T>(d), stage_bytes = 2 * AG_TN * pitch;
     float *q_s = reinterpret_cast<float *>(ag_smem_base + AG_STAGES * stage_bytes);
     float *x_s = reinterpret_cast<float *>(ag_smem_base);   // at the end, over the tiles: [4 warps][4 rows][d], sums of warps that share rows
@@ -56,7 +56,7 @@ template <typename T, int DD> __global__ void __launch_bounds__(AG_THREADS, 3) a
     AttnSegment g;
     walk.begin(p, cta, AG_M, AG_TN);
     while (walk.next(p, cta, AG_M, AG_TN, g)) {
-        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up, &tree_good)) {
+        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up)) {
             if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
             continue;
         }

@@ -42,7 +42,7 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
     constexpr int M = 16 * WM, WN = 4 / WM, TW = AR_TN / WN, NB = TW / 8, KS = D / 16, PIECES = D / 8;
     extern __shared__ __align__(128) unsigned char ar_base[];
     __shared__ unsigned long long anc[AT_SMALL_ROWS];
-    __shared__ int anc_up[AT_SMALL_ROWS], tree_good;
+    __shared__ int anc_up[AT_SMALL_ROWS];
     __shared__ long long off_s[4][AR_TN];
     __shared__ float ml_s[4][16][2];
     __shared__ int odd_s;   // some value of this call's rows is infinite or no number
@@ -56,7 +56,7 @@ template <int D, int WM> __global__ void __launch_bounds__(AR_THREADS, ar_ctas<D
     AttnSegment g;
     walk.begin(p, cta, M, AR_TN);
     while (walk.next(p, cta, M, AR_TN, g)) {
-        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up, &tree_good)) {
+        if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, g.s, anc, anc_up)) {
             if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
             continue;
         }

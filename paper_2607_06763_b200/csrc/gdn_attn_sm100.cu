@@ -39,7 +39,7 @@ struct UnitShared {
     int anc_up[AT_SMALL_ROWS];
     unsigned long long q_full, k_full[AS_MOST], v_full[AS_MOST], v_landed[AS_MOST], k_empty[AS_MOST], v_empty[AS_MOST], s_full[2], p_full[2][2], o_full[2];   // p_full: [half of the tile][stream]
     uint32_t tmem;
-    int odd, dead, good;
+    int odd, dead;
 };
 
 // Byte offset of 16-byte piece c of row r of a [128][D] operand tile: [D / 64][128 rows][128 bytes], swizzled.
@@ -218,7 +218,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
             if (!walk.next(p, cta, AS_M, AS_TN, t.g)) return false;
             __syncthreads();   // the unit before is through
             if (*dead) return false;
-            if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, t.g.s, sh.anc, sh.anc_up, &sh.good)) {
+            if (p.row_offsets && kind == AT_WORDS64 && !attn_ancestors(p, t.g.s, sh.anc, sh.anc_up)) {
                 if (tid == 0) report_status(p.status_dev, GDN_ERR_TREE);
                 continue;
             }

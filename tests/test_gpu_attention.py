@@ -597,3 +597,28 @@ def test_decode_steps_as_a_model_runs_them(cuda_device):
     for b in range(B):
         assert int(seq_lens[b]) == len(tokens[b])
         check_against_dense(b, o[b], tokens[b])
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,dtype", [(4, 4, 64, "bf16"), (8, 2, 128, "bf16"), (6, 2, 40, "bf16"), (4, 2, 64, "f32")])
+@pytest.mark.parametrize("rows", [7, 64])
+def test_bad_trees_between_good_ones(cuda_device, rows, h_q, h_kv, d, dtype):
+    """Runs of many short units, every second of them of a tree that is none: what one unit's check of its tree says must not be
+    taken for the next one's by any warp."""
+    rng = np.random.default_rng(40)
+    n = 300
+    c = Call(41, [int(x) for x in rng.integers(0, 200, n)], [rows] * n, h_q, h_kv, d, dtype, slack=20)
+    broken = [b for b in range(n) if b % 2 == 1 and b % 5 != 0]
+    for b in broken:
+        c.parent[int(c.offsets[b]) + rows - 1] = rows
+    good = [b for b in range(n) if b not in broken]
+    for _ in range(5):
+        c.o.fill_(7.0)
+        c.status.zero_()
+        assert c.run() == 0 and c.device_status() == -7
+    c.check(only=good[::7])
+    first = c.o.clone()
+    for b in broken:
+        assert bool((first[int(c.offsets[b]):int(c.offsets[b + 1])] == 7.0).all())
+    c.o.fill_(7.0)
+    assert c.run() == 0 and c.device_status() == -7
+    assert bool((first == c.o).all())
