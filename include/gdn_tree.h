@@ -440,6 +440,8 @@ int gdn_attn_decode(const gdn_attn_shape_t *shape, const void *q, const void *k_
  * Attention of the nodes of a draft tree (or of a chunk of a prompt, parent NULL): row i of sequence b sees its seq_lens[b]
  * committed tokens, its ancestors and itself, row j being token seq_lens[b] + j of the cache, where gdn_kv_append put it.
  * Nodes that a row does not see have no influence on it, whatever their values.
+ * (Both calls.)  Among what a row sees, a score that is NaN or +inf makes its output NaN, as inf - inf is none; a score of -inf weighs
+ * nothing, and where all of them are -inf the row gets zeros, as one that sees nothing.
  */
 int gdn_attn_tree_verify(const gdn_attn_shape_t *shape, const void *q, const void *k_cache, const void *v_cache,
                          const int32_t *page_table, const int32_t *seq_lens, const int32_t *parent,

@@ -136,7 +136,8 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b)
 // 2^x of two numbers of at most 2^7 without the special function unit, which forms 16 per clock and SM where a tile pair's products
 // leave time for 32768 / 2048: x = n + r, |r| <= 1/2, 2^r by the polynomial of degree 3 with p(0) = 1 that is off by the least
 // relative error there, 1.0e-4 (fitted to 2^r; a twentieth of the step of the bf16 weights), and n into the exponent.  Below
-// 2^-126 the result stays there: not for scores that are hidden.
+// 2^-126 the result stays there, and so it does for what is no number: not for scores that are hidden, and not for a tile of a row whose
+// largest score is infinite or among whose scores one is no number.
 __device__ __forceinline__ float2 power_of_two_by_products(float2 x)
 {
     x.x = fmaxf(x.x, -126.f);
@@ -148,6 +149,14 @@ __device__ __forceinline__ float2 power_of_two_by_products(float2 x)
     y = fma2(r, y, make_float2(0.6932829022407532f, 0.6932829022407532f));
     y = fma2(r, y, make_float2(1.f, 1.f));
     return make_float2(__int_as_float(__float_as_int(y.x) + (__float_as_int(n.x) << 23)), __int_as_float(__float_as_int(y.y) + (__float_as_int(n.y) << 23)));
+}
+
+// The largest of three; no number where one of them is none.
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // What all warps know of the unit at hand.
@@ -294,13 +303,15 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
 #pragma unroll
                     for (int j = 0; j < 128; j += 8)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) t4[k] = fmaxf(fmaxf(t4[k], __uint_as_float(x[j + k])), __uint_as_float(x[j + 4 + k]));
-                    const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+                        for (int k = 0; k < 4; ++k) t4[k] = max3_nan(t4[k], __uint_as_float(x[j + k]), __uint_as_float(x[j + 4 + k]));
+                    const float top = max3_nan(max3_nan(t4[0], t4[1], t4[2]), t4[3], t4[3]);
+                    // some score is +inf or no number, or all are -inf: the differences to the maximum may be no numbers, and stay that
+                    const bool odd_scores = __any_sync(0xffffffffu, !(fabsf(top) < INFINITY));
                     const bool first = i == 0;
                     const bool raise = first || (top - m) * p.scale_log2 > AS_SLACK || (m == -INFINITY && top > -INFINITY);
                     float fade = 1.f;
                     if (raise) {
-                        const float m_new = fmaxf(m, top);
+                        const float m_new = fmaxf(m, top);   // (of a number and none, the number)
                         fade = first || m == -INFINITY ? 0.f : power_of_two((m - m_new) * p.scale_log2);
                         m = m_new;
                         l *= fade;
@@ -333,7 +344,7 @@ attn_sm100_kernel(const AttnParams p, const __grid_constant__ CacheMaps maps)
                                 w[j] = pack_bf16(e.x, e.y);
                             }
                         };
-                        if (hidden) weights(No{});
+                        if (hidden || odd_scores) weights(No{});
                         else weights(Yes{});
                         GDN_TMEM_ST16(s_at + c * 16, w);
                         if (c == 1 || c == 3) {   // half of the tile's weights: their part of the second product may begin

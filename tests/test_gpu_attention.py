@@ -622,3 +622,54 @@ def test_bad_trees_between_good_ones(cuda_device, rows, h_q, h_kv, d, dtype):
     c.o.fill_(7.0)
     assert c.run() == 0 and c.device_status() == -7
     assert bool((first == c.o).all())
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,dtype,rows,chain", [(8, 1, 128, "bf16", 3, False), (8, 1, 64, "bf16", 8, True), (8, 1, 128, "bf16", 40, False),
+                                                         (8, 1, 64, "bf16", 70, True), (2, 1, 128, "bf16", 200, True), (4, 2, 64, "f32", 5, False),
+                                                         (4, 2, 40, "bf16", 20, True)])
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")], ids=str)
+def test_committed_keys_that_are_no_numbers(cuda_device, h_q, h_kv, d, dtype, rows, chain, value, many):
+    """One component of one committed key, at each place modulo 16 of tiles that all rows see: a row whose score there is +inf or NaN
+    is NaN (inf - inf, as in 64 bits), one whose score is -inf is what it is without the token.  In units that several runs share, and
+    (many) in units of one run."""
+    n, L, e = (320, 150, 5) if many else (17, 400, 5)
+    lens = [L] * (n - 1) + [150 if many else 3000]
+    c = Call(42, lens, [rows] * n, h_q, h_kv, d, dtype, chain=chain)
+    at_ = [b % 128 for b in range(n)] if many else [129 + b if b % 2 else b for b in range(n - 1)] + [1500]
+    clean = []
+    for b in range(n):
+        k, v = c.cache.read(b, c.held[b])
+        clean.append((k.copy(), v))
+        k[at_[b], :, e] = value
+        c.cache.write(b, k, v)
+    assert c.run() == 0 and c.device_status() == 0
+    got = c.o.double().cpu().numpy()
+    for b in range(n) if rows <= 8 and not many else range(40, 60) if rows <= 40 and many else range(0, n, n // 5):
+        q = c.q64[c.offsets[b]:c.offsets[b + 1]]
+        o = got[c.offsets[b]:c.offsets[b + 1]]
+        gone = q[..., e] * value == -np.inf          # (nothing else is: a query's component is 0 nowhere)
+        assert (np.isnan(o).all(-1) == ~gone).all() and (np.isfinite(o).all(-1) == gone).all(), b
+        k, v = clean[b]
+        see = c.see(b)
+        see[:, at_[b]] = False
+        want, a, big = at.attend(q, k, v, see, c.scale)
+        assert (np.abs(o - want) <= at.allowed(want, a, big, dtype, d, c.held[b]))[gone].all(), b
+
+
+@pytest.mark.parametrize("h_q,h_kv,d,dtype,rows", [(8, 1, 128, "bf16", 3), (8, 1, 128, "bf16", 40), (8, 1, 64, "bf16", 70), (4, 2, 64, "f32", 5),
+                                                   (4, 2, 40, "bf16", 20)])
+@pytest.mark.parametrize("n", [1, 150])
+def test_rows_whose_scores_are_all_minus_infinity(cuda_device, h_q, h_kv, d, dtype, rows, n):
+    """Zeros, as where a row sees nothing; where they are all +inf, NaN."""
+    c = Call(43, [300, 0, 2000] if n == 1 else [140] * n, [rows] * (3 if n == 1 else n), h_q, h_kv, d, dtype)
+    c.q[:, :, 7] = -1.0
+    c.q[::3, :, 7] = 1.0
+    for b in range(len(c.lens)):
+        k, v = c.cache.read(b, c.held[b])
+        k[..., 7] = -np.inf
+        c.cache.write(b, k, v)
+    assert c.run() == 0 and c.device_status() == 0
+    got = c.o[:c.N].double().cpu().numpy()
+    assert (got[::3] == 0.0).all()
+    assert np.isnan(np.delete(got, np.arange(0, c.N, 3), 0)).all()
