@@ -16,10 +16,10 @@
 // to the bin, warp by warp, also says where the token lies.
 // The first k of a row, k up to two thousand, are put in order at once, and the row is done with.
 //
-// A token on the wrong side of a border is another token, so that weights are summed as integers, in units of 2^-38 (no order
-// of additions matters).  Those that make up more than about a thousandth of everything (where that is not known, those of 2^-6 and more)
-// are formed to about 1e-9 of themselves, the others to fp32: their errors are as often up as down, and 2^-34 of everything at most.  The difference m - x is kept in two parts, and so is 1 / T.  Tokens more than 39 powers of two
-// below the top weigh less than a unit, and nothing.
+// A token on the wrong side of a border is another token, so that weights are formed in 64 bits (to 2e-12 of themselves) and summed as
+// integers, in units of 2^-45, where no order of additions matters: 2^18 weights of 1 just fit.  Each is rounded to whole units, which makes
+// the sum of n of them wrong by n 2^-46 at most (equal logits), as a rule by sqrt(n) 2^-47; less than half a unit is nothing.  (In fp32 a
+// weight is off by up to 2^-24 of itself, and the sum of many that are alike by as much.)
 #include <cooperative_groups.h>
 
 #include "gdn_attn.cuh"
@@ -36,25 +36,11 @@ constexpr int SA_BINS = 2048, SA_OWN = SA_BINS / SA_THREADS;   // bins, of a thr
 constexpr int SA_HELD = 32 << 10;       // bytes of a row that a CTA holds in shared memory
 constexpr float SA_PER_NAT = 64.f;
 constexpr int SA_SORT = 2048;           // members of a bin that are sorted; more are bisected, which takes some 40 passes: 0.7 ms for 131071 logits
-constexpr int SA_UNIT = 38;             // weights in units of 2^-38
-constexpr float SA_COARSE = 6.f;        // weights below 2^-6 are formed to fp32, where nothing is known of their sum
-constexpr float SA_LAST = 42.f;         // a weight of 2^-42 is none
+constexpr int SA_UNIT = 45;             // weights in units of 2^-45
+constexpr double SA_DEEP = 60.0;        // logits further below the largest than this many powers of two count as that far: weights of nothing
 typedef unsigned long long u64;
 
-// 2^(38 - j/32), rounded.
-__constant__ u64 powers[32] = {
-    274877906944ull, 268987840221ull, 263223985481ull, 257583638263ull,
-    252064152055ull, 246662937055ull, 241377458955ull, 236205237751ull,
-    231143846582ull, 226190910588ull, 221344105800ull, 216601158044ull,
-    211959841877ull, 207417979546ull, 202973439958ull, 198624137689ull,
-    194368031998ull, 190203125877ull, 186127465105ull, 182139137339ull,
-    178236271212ull, 174417035459ull, 170679638052ull, 167022325365ull,
-    163443381347ull, 159941126720ull, 156513918187ull, 153160147665ull,
-    149878241531ull, 146666659877ull, 143523895795ull, 140448474667ull};
-
 struct SampleShared {
-    u64 table[32];                      // `powers`
-    float table_4[32];                  // the same in units of 4
     u64 sorted[SA_SORT];                // members of a bin; of rank 0, those of all ranks
     uint32_t count[SA_BINS + 32];       // of the CTA; then, for the bins of this rank's share, of the cluster; 32 for what lies behind all bins
     u64 sum[2][5][SA_WARPS + 1];        // of the CTA's warps, then of the CTA (read by the cluster), in turn
@@ -69,34 +55,42 @@ struct SampleShared {
     bool few;                           // tokens down to the end of `bin`
 };
 
-// Weight of the token with logit x in units, to about 1e-9 of itself, whatever its size (see Weigh).  A function of its own, as the other
-// steps that are taken now and then are: inlined wherever they are called they make code that few rows never find in the
-// instruction cache.
-__device__ __noinline__ u64 weigh_finely(float x, float m, float per_hi, float per_lo, const u64 *table, const float *table_4)
+// 2^(d per) in units, d per in [-62, 0]: n + r with r in [-1/2, 1/2], 2^r by the polynomial of degree 8 with p(0) = 1 and the least relative
+// error there, 1.1e-12 (fitted to 2^r), n into the exponent; a number so large that its last bit is a unit rounds to whole units and leaves
+// them in the low bits.  (Doubles run at half of fp32's rate, but need half the instructions that fp32 in two parts, to 8e-8, did: 256 x
+// 131071 logits without filters 105 us instead of 153, with top-p 230 either way.)
+__device__ __forceinline__ u64 units_of_power(double d, double per)
 {
-    if (x == m) return 1ull << SA_UNIT;
-    const float d = m - x;
-    if (!(d * per_hi < SA_LAST && d < INFINITY)) return 0;
-    // m - x = d + lo exactly
-    const float back = d - m, lo = (m - (d - back)) + (-x - back);
-    const float t = __fmul_rn(d, per_hi);   // (rounded here, whatever is added to it: err is what this loses)
-    const float err = fmaf(lo, per_hi, fmaf(d, per_hi, -t) + d * per_lo);
-    const float t32 = t * 32.f;
-    const float shifted = t32 + 12582912.f;                 // 1.5 * 2^23: rounds to a whole number
-    const int n = __float_as_int(shifted) - 0x4B400000;
-    const float r = -((t32 - (shifted - 12582912.f)) + 32.f * err) * 0.021660849392498290f;   // ln(2) / 32
-    // e^r - 1 of |r| <= 0.011: the terms of its series
-    const float q = r * fmaf(r, fmaf(r, fmaf(r, 0.041666666666666664f, 0.16666666666666666f), 0.5f), 1.f);
-    // (the correction is below 2^38 * 0.011 < 2^32: in units of 4 it fits a 32-bit number)
-    const u64 v = table[n & 31] + (u64)((long long)__float2int_rn(table_4[n & 31] * q) * 4);
-    const int down = n >> 5;
-    return down ? (v + (1ull << (down - 1))) >> down : v;
+    constexpr double whole = 6755399441055744.0;                             // 1.5 * 2^52
+    constexpr double unit = 1.5 * (double)(1ull << (52 - SA_UNIT));
+    const double n = fma(d, per, whole), r = fma(d, per, whole - n);
+    double y = 1.3344183484134179e-06;
+    y = fma(y, r, 1.5314209223349525e-05);
+    y = fma(y, r, 0.0001540309828656179);
+    y = fma(y, r, 0.0013333434157560176);
+    y = fma(y, r, 0.009618129558838935);
+    y = fma(y, r, 0.05550410959228811);
+    y = fma(y, r, 0.2402265069474259);
+    y = fma(y, r, 0.6931471805412327);
+    y = fma(y, r, 1.0);
+    y = __hiloint2double(__double2hiint(y) + (__double2loint(n) << 20), __double2loint(y));
+    return (u64)(__double_as_longlong(y + unit) - __double_as_longlong(unit));
+}
+
+// Weight in units of any logit, where the largest is so large, or weights fall so slowly or so fast, that Weigh's bound is none.  A
+// function of its own, as the other steps that are taken now and then are: inlined wherever they are called they make code that few rows
+// never find in the instruction cache.
+__device__ __noinline__ u64 weigh_any(float x, double m, double per)
+{
+    if (!(x > -INFINITY)) return 0;   // (no number, too)
+    const double d = (double)x - m;
+    return d * per > -SA_DEEP ? units_of_power(d, per) : 0;
 }
 
 // The same without the unit's rounding, of one token that weighs something.
-__device__ __noinline__ double weigh_exactly(float x, float m, float per_hi, float per_lo)
+__device__ __noinline__ double weigh_exactly(float x, double m, double per)
 {
-    return (x == m ? 1.0 : exp(((double)x - (double)m) * ((double)per_hi + (double)per_lo) * 0.6931471805599453)) * (double)(1ull << SA_UNIT);
+    return exp(((double)x - m) * per * 0.6931471805599453) * (double)(1ull << SA_UNIT);
 }
 
 // By a whole CTA: `have` keys in rising order, by exchanges at distances that are powers of two; the greatest number stands behind them
@@ -122,50 +116,24 @@ __device__ __noinline__ void sort_keys(u64 *keys, int have)
         }
 }
 
-// Weights in units of tokens with given logits; per = log2(e) / T in two parts.
+// Weights in units of tokens with given logits.
 struct Weigh {
-    float m, per_hi, per_lo;
-    float x_fine, x_last;   // logits above the first are weighed finely; below the last nothing is left
-    bool all_fine;
-    const u64 *table;
-    const float *table_4;
+    double m, per;   // the largest logit; log2(e) / T
+    float deep;      // logits below count as this one, which weighs nothing
+    bool any;        // no such bound: see weigh_any
 
-    __device__ __forceinline__ u64 fine(float x) const { return weigh_finely(x, m, per_hi, per_lo, table, table_4); }
-    // To fp32, where x < x_fine (anything elsewhere).  (Two at a time by packed operations, each constant would take two registers.)
-    __device__ __forceinline__ u64 coarse(float x) const
-    {
-        x = fmaxf(x, x_last);   // (no number, too)
-        const float d = m - x;
-        const float lo = (m - d) - x;   // what the difference loses, where |x| <= m
-        const float t = __fmul_rn(d, -per_hi);
-        const float e = fmaf(lo, per_hi, fmaf(d, per_lo, fmaf(d, per_hi, t)));
-        const float n = t + 12582912.f;
-        const float r = (t - (n - 12582912.f)) - e;
-        // 2^r on [-1/2, 1/2]: the polynomial of degree 6 with the least relative error, 2e-9 (fitted to 2^r), to fp32
-        float q = fmaf(r, 0.0001534581242594868f, 0.0013399930903688073f);
-        q = fmaf(r, q, 0.009618489071726799f);
-        q = fmaf(r, q, 0.05550328642129898f);
-        q = fmaf(r, q, 0.24022646248340607f);
-        q = fmaf(r, q, 0.6931471824645996f);
-        q = fmaf(r, q, 1.f);
-        return __float2ull_rn(__int_as_float(__float_as_int(q) + (__float_as_int(n) << 23) + (SA_UNIT << 23)));   // (0x4B400000 << 23 is 0)
-    }
+    __device__ __forceinline__ u64 one(float x) const { return weigh_any(x, m, per); }
     __device__ __forceinline__ void four(const float4 &x, u64 (&w)[4]) const
     {
-        if (all_fine) {
+        if (any) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = fine((&x.x)[j]);
+            for (int j = 0; j < 4; ++j) w[j] = one((&x.x)[j]);
             return;
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = coarse((&x.x)[j]);
-        if (fmaxf(fmaxf(x.x, x.y), fmaxf(x.z, x.w)) > x_fine) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if ((&x.x)[j] > x_fine) w[j] = fine((&x.x)[j]);
-        }
+        for (int j = 0; j < 4; ++j) w[j] = units_of_power((double)fmaxf((&x.x)[j], deep) - m, per);   // (of a number and none, the number)
     }
-    __device__ __forceinline__ double exactly(float x) const { return weigh_exactly(x, m, per_hi, per_lo); }
+    __device__ __forceinline__ double exactly(float x) const { return weigh_exactly(x, m, per); }
 };
 
 __device__ __forceinline__ uint32_t ordered(float x)   // as unsigned numbers in the order of x
@@ -204,10 +172,6 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
     const int row = (int)blockIdx.x / ranks;
     constexpr int PIECE = 16 / (int)sizeof(T);
 
-    if (tid < 32) {
-        sh.table[tid] = powers[tid];
-        sh.table_4[tid] = (float)powers[tid] * 0.25f;
-    }
     if (tid == 0) sh.members = 0;
     for (int i = tid; i < SA_BINS; i += SA_THREADS) sh.count[i] = 0;
     wait_for_previous_kernel();
@@ -338,12 +302,10 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
     if (k >= p.vocab) k = 0;
     const float top_p = p.top_p ? p.top_p[row] : 1.f, min_p = p.min_p ? p.min_p[row] : 0.f;
     const bool by_k = k > 0, by_p = top_p < 1.f;
-    const double per = fmin(1.4426950408889634 / (double)T_row, 1e30);
-    const float per_hi = (float)per, per_lo = (float)(per - (double)per_hi), d_last = SA_LAST / per_hi;
-    // where logits lie so far apart that x_last cannot be told from m, or weights fall so slowly that differences overflow, all are weighed
-    // finely
-    Weigh weigh{m, per_hi, per_lo, m - SA_COARSE / per_hi, m - d_last,
-                      !(fabsf(m) * 2.4e-7f < 0.1f * d_last && fabsf(m) + d_last < 1e37f), sh.table, sh.table_4};
+    const double per = 1.4426950408889634 / (double)T_row;
+    const float d_deep = (float)(SA_DEEP / per);
+    // (the bound can be told from m, and is finite)
+    const Weigh weigh{m, per, m - d_deep, !(fabsf(m) * 2.4e-7f < 0.1f * d_deep && fabsf(m) + d_deep < 1e37f)};
     const float to_bin = (float)fmin((double)SA_PER_NAT / (double)T_row, 1e30);
     auto place_of = [&](float x) { return (m - x) * to_bin; };   // its whole part is the bin; it falls as x rises (no number: in no bin)
 
@@ -458,7 +420,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                     u64 own_w[OWN], upto = 0;
 #pragma unroll
                     for (int j = 0; j < OWN; ++j) {
-                        own_w[j] = weights && tid * OWN + j < have ? weigh.fine(logit_of(sh.sorted[tid * OWN + j])) : 0;
+                        own_w[j] = weights && tid * OWN + j < have ? weigh.one(logit_of(sh.sorted[tid * OWN + j])) : 0;
                         upto += own_w[j];
                     }
                     u64 sum = upto;
@@ -500,7 +462,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                             const float x = (&v.x)[j], b = place_of(x);
                             if (in_bin(b, bin) && key_of(x, index_at(i + j)) <= mid && inside(b, x, i + j)) {
                                 ++a[1];
-                                if (weights) a[0] += weigh.fine(x);
+                                if (weights) a[0] += weigh.one(x);
                             }
                         }
                     });
@@ -552,7 +514,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                         bool over = false;
                         for (int i = 0; i < k && !over; i += 32) {
                             const bool there = i + lane < k;
-                            u64 upto = there ? weigh.fine(logit_of(sh.sorted[i + lane])) : 0;
+                            u64 upto = there ? weigh.one(logit_of(sh.sorted[i + lane])) : 0;
                             const u64 own_w = upto;
 #pragma unroll
                             for (int off = 1; off < 32; off <<= 1) {
@@ -585,7 +547,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                 if (warp == 0) {
                     auto logit_at = [&](int i) { return logit_of(sh.sorted[i] << 32); };
                     u64 z = 0;
-                    for (int i = lane; i < kept_n; i += 32) z += weigh.fine(logit_at(i));
+                    for (int i = lane; i < kept_n; i += 32) z += weigh.one(logit_at(i));
 #pragma unroll
                     for (int off = 16; off; off >>= 1) z += __shfl_xor_sync(0xffffffffu, z, off);
                     double u = (double)p.uniform[row];
@@ -595,7 +557,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                     u64 sum = 0;
                     for (int i = 0; i < kept_n; i += 32) {
                         const float x = i + lane < kept_n ? logit_at(i + lane) : -INFINITY;
-                        const u64 own_w = i + lane < kept_n ? weigh.fine(x) : 0;
+                        const u64 own_w = i + lane < kept_n ? weigh.one(x) : 0;
                         u64 upto = own_w;
 #pragma unroll
                         for (int off = 1; off < 32; off <<= 1) {
@@ -651,8 +613,6 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
             }
             float estimate = 0.f;   // of everything
             for (int i = 0; i < SA_WARPS; ++i) estimate += sh.scan_a[i];
-            // finely weighed: what makes up more than about a thousandth of everything
-            weigh.x_fine = m - fminf(fmaxf((float)(SA_UNIT + 10) - log2f(estimate), 0.f), SA_LAST) / per_hi;
             // the first bin in (from, to) that has members of the prefix and up to whose end about `goal` has gathered; else the last, or -1
             auto search = [&](int from, int to, float goal) {
                 __syncthreads();
@@ -757,7 +717,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
                         const u64 member = list[i];
                         const int index = (int)(uint32_t)member;
                         if (member <= key && index >= index_at(from_place) && index < index_at(to_place) && index >= first && index < first + n) {
-                            const u64 ww = weigh.fine(logit_of(member));
+                            const u64 ww = weigh.one(logit_of(member));
                             if (ww >= least) w += ww;
                         }
                     }
@@ -783,9 +743,7 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float b = place_of((&v.x)[j]);
-                if (b < cut_from) continue;
-                // (members of the last bin are weighed as the list's are)
-                own[j] = b < cut_behind && key_of((&v.x)[j], index_at(place + j)) <= cut_key ? weigh.fine((&v.x)[j]) : 0;
+                if (!(b < cut_from || (b < cut_behind && key_of((&v.x)[j], index_at(place + j)) <= cut_key))) own[j] = 0;
             }
         }
         if (least) {

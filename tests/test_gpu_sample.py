@@ -152,3 +152,77 @@ def test_captured_sampling_follows_its_arrays(cuda_device):
         got = token.cpu().numpy()
         for r in range(6):
             assert got[r] == at.sample(x[r].double().cpu().numpy(), float(u[r]), p=float(p[r]))[0]
+
+
+def _next_to_borders(cum, bound, rng, n, low=0.0):
+    """Random numbers (fp32) that lie `bound` to 4 `bound` of the sum behind, or in front of, the end of a token's interval."""
+    z = cum[-1]
+    out = []
+    for j in rng.permutation(len(cum) - 1):
+        near = np.float32(cum[j] / z)
+        for u in (near, np.nextafter(near, np.float32(0)), np.nextafter(near, np.float32(1))):
+            if low <= u < 1.0 and bound < abs(float(u) - cum[j] / z) < 4 * bound:
+                out.append(u)
+                break
+        if len(out) == n:
+            return np.array(out, np.float32)
+    raise AssertionError("too few")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [0.0, -3.0, 5.0], ids=str)
+def test_random_numbers_next_to_a_tokens_end(cuda_device, dtype, top):
+    """A likely token behind a hundred thousand unlikely ones of few values, so that errors of their weights add up.  Each weight may be
+    off by 2^-46 of the likeliest one's (half a unit), all of them together by vocab 2^-46: tokens are the ones of 64 bits wherever the
+    random number is further than that from a border."""
+    import torch
+    n, vocab = 24, 100003
+    rng = np.random.default_rng(50)
+    x = torch.empty(n, vocab, dtype=at.torch_dtype(dtype), device="cuda")
+    u = np.zeros(n, np.float32)
+    for r in range(n):
+        values = torch.from_numpy(top - rng.uniform(9.0, 12.5, 1 if r % 2 else 5)).to(x.dtype)
+        row = values[torch.from_numpy(rng.integers(0, len(values), vocab))]
+        row[-1] = top
+        x[r] = row.cuda()
+        w = np.exp(row.double().numpy() - top)
+        cum = np.cumsum(w)
+        u[r] = _next_to_borders(cum, vocab * 2.0 ** -46 / cum[-1], rng, 1)[0]
+    _check(x, u)
+
+
+def test_random_numbers_next_to_a_tokens_end_in_spread_logits(cuda_device):
+    """Logits of a normal distribution, positive and negative ones, far below zero (log-probabilities) too."""
+    import torch
+    n, vocab = 24, 50000
+    rng = np.random.default_rng(51)
+    x = 2.2 * rng.standard_normal((n, vocab))
+    x[8:16] -= 11.0
+    x[16:] = x[16:] - np.log(np.exp(x[16:]).sum(1, keepdims=True))
+    x = torch.from_numpy(x).float().cuda()
+    u = np.zeros(n, np.float32)
+    for r in range(n):
+        row = x[r].double().cpu().numpy()
+        cum = np.cumsum(np.exp(row - row.max()))
+        u[r] = _next_to_borders(cum, vocab * 2.0 ** -46 / cum[-1], rng, 1)[0]
+    _check(x, u)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_filters_that_end_next_to_a_border(cuda_device, dtype):
+    """top_p just in front of, or behind, the share at which a prefix has one token more."""
+    import torch
+    n, vocab = 24, 60000
+    rng = np.random.default_rng(52)
+    x = torch.from_numpy(1.5 * rng.standard_normal((n, vocab)) - np.where(np.arange(n) % 2, 9.0, 0.0)[:, None]).to(at.torch_dtype(dtype)).cuda()
+    p, u = np.zeros(n, np.float32), np.zeros(n, np.float32)
+    for r in range(n):
+        row = x[r].double().cpu().numpy()
+        order = np.argsort(-row, kind="stable")
+        w = np.exp(row[order] - row[order[0]])
+        cum, bound = np.cumsum(w), vocab * 2.0 ** -46
+        p[r] = _next_to_borders(cum, bound / cum[-1], rng, 1, 0.3)[0]
+        kept = np.sort(order[:int(np.searchsorted(cum, float(p[r]) * cum[-1])) + 1])
+        mass = np.cumsum(np.exp(row[kept] - row[order[0]]))
+        u[r] = _next_to_borders(mass, bound / mass[-1], rng, 1)[0]
+    _check(x, u, None, None, p)
