@@ -468,7 +468,9 @@ typedef struct gdn_sample_shape {
  *   uniform      [device] fp32 [n_rows] in [0, 1) (clamped to it; NaN: 0)
  *   temperature <= 0 or NaN: the largest logit, the lowest index among equals, prob 1; top_k <= 0 or >= vocab, top_p >= 1 or NaN,
  *   min_p <= 0 or NaN: off.  A logit of -inf or NaN is never taken; one of +inf is taken before all finite ones.  A row without any logit that
- *   can be taken gives token -1, prob 0.  Tokens whose weight is below 2^-41 of the likeliest one's are not taken.
+ *   can be taken gives token -1, prob 0.  Weights (exp of the difference to the largest logit / temperature) count in units of
+ *   2^-45 of the likeliest one's, each rounded, so that a token of less than half a unit is not taken, and a random number, top_p or
+ *   min_p within vocab * 2^-46 of a border may fall on its other side.
  * status_dev is not written by this build.
  */
 int gdn_sample(const gdn_sample_shape_t *shape, const void *logits, const float *temperature, const int32_t *top_k,

@@ -226,3 +226,24 @@ def test_filters_that_end_next_to_a_border(cuda_device, dtype):
         mass = np.cumsum(np.exp(row[kept] - row[order[0]]))
         u[r] = _next_to_borders(mass, bound / mass[-1], rng, 1)[0]
     _check(x, u, None, None, p)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tokens_far_below_the_likeliest(cuda_device, dtype):
+    """Weights down to 2^-45 of the likeliest one's are taken (half a unit of 2^-45 is rounded off); what is below 2^-46 is not."""
+    import torch
+    n, vocab = 8, 3000
+    nats = np.array([26.5, 27.0, 27.5, 28.0, 28.25, 28.5, 29.0, 30.5])
+    x = torch.full((n, vocab), -40.0, dtype=at.torch_dtype(dtype), device="cuda")
+    x[:, 1] = torch.from_numpy(-nats).to(x.dtype).cuda()
+    x[:, -1] = 0.0
+    w = np.exp(x[:, 1].double().cpu().numpy())
+    _check(x, 0.5 * w)           # inside the interval of token 1, for what lies in front of it weighs nothing
+    _check(x, 2.0 * w)           # behind it
+    far = torch.full((2, vocab), -32.0, dtype=x.dtype, device="cuda")     # 2^-46.2 each
+    far[:, -1] = 0.0
+    status, token = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    import paper_2607_06763_b200 as gdn
+    assert gdn.gdn_sample(gdn.GdnSampleShape.from_logits(far), far, None, None, None, None, torch.tensor([0.0, 1e-13], device="cuda"), token, None,
+                          status) == 0
+    assert token.tolist() == [vocab - 1] * 2
