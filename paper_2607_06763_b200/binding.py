@@ -101,21 +101,52 @@ class GdnAttnShape(ctypes.Structure):
     @classmethod
     def from_cache(cls, k_cache, page_table, h_q: int, total_rows: int, max_rows: int, max_len: int | None = None,
                    scale: float | None = None, q_stride: int | None = None, k_stride: int | None = None,
-                   v_stride: int | None = None) -> "GdnAttnShape":
+                   v_stride: int | None = None, *, v_cache=None, q=None, k=None, v=None, seq_lens=None) -> "GdnAttnShape":
         """Shape of calls on a cache seen as ``[page][token][head][component]`` (any strides; the value cache has the same) with
         ``page_table`` ``[n_seq][max_pages]``.  ``max_len`` defaults to all that a row of the table can hold, ``scale`` to
-        ``1/sqrt(d)``, the row strides to packed rows."""
+        ``1/sqrt(d)``, the row strides to packed rows.
+
+        The calls themselves take addresses and look at no tensor.  What they will be given can be given here by keyword: the row strides
+        are then those of ``q``, ``k``, ``v`` (``[rows][heads][d]``, or ``[rows][any]`` for slices of a fused projection), and a value
+        cache that does not lie as the key cache does, rows of another type or with heads apart, and lengths that are not int32 are a
+        ``ValueError``."""
         n_pages, page_size, h_kv, d = k_cache.shape
         if k_cache.stride(3) != 1:
             raise ValueError("the components of a head must be contiguous")
         dtype = {"torch.float32": GDN_F32, "torch.bfloat16": GDN_BF16}.get(str(k_cache.dtype))
         if dtype is None:
             raise ValueError(f"the cache is fp32 or bf16, not {k_cache.dtype}")
+        if v_cache is not None and (v_cache.dtype != k_cache.dtype or v_cache.shape != k_cache.shape or
+                                    any(n > 1 and a != b for n, a, b in zip(k_cache.shape, k_cache.stride(), v_cache.stride()))):
+            raise ValueError("the value cache must have the key cache's type, sizes and strides")
+        for name, ints in (("page_table", page_table), ("seq_lens", seq_lens)):
+            if ints is None:
+                continue
+            contiguous = ints.is_contiguous() if hasattr(ints, "is_contiguous") else ints.flags.c_contiguous
+            if str(ints.dtype).rpartition(".")[2] != "int32" or not contiguous:
+                raise ValueError(f"{name} must be contiguous int32, not {ints.dtype}")
+        if len(page_table.shape) != 2 or (seq_lens is not None and tuple(seq_lens.shape) != (page_table.shape[0],)):
+            raise ValueError("page_table is [n_seq][max_pages], seq_lens [n_seq]")
+
+        def row_stride(name, rows, given, heads):
+            if rows is None:
+                return heads * d if given is None else given
+            if rows.dtype != k_cache.dtype or rows.dim() not in (2, 3) or rows.stride(-1) != 1:
+                raise ValueError(f"{name} must be contiguous rows of the cache's type")
+            if rows.dim() == 3 and (tuple(rows.shape[1:]) != (heads, d) or (heads > 1 and rows.stride(1) != d)):
+                raise ValueError(f"{name} must be [rows][{heads}][{d}] with the heads of a row side by side")
+            if rows.dim() == 2 and rows.shape[1] < heads * d:
+                raise ValueError(f"rows of {name} have {heads} heads of {d} components")
+            stride = rows.stride(0) if rows.shape[0] > 1 else heads * d if given is None else given
+            if given is not None and stride != given:
+                raise ValueError(f"rows of {name} lie {stride} elements apart, not {given}")
+            return stride
+
         n_seq, max_pages = page_table.shape
         return cls(n_seq, h_q, h_kv, d, dtype, total_rows, max_rows, n_pages, page_size, max_pages,
                    max_pages * page_size if max_len is None else max(1, max_len), d ** -0.5 if scale is None else scale,
-                   k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), h_q * d if q_stride is None else q_stride,
-                   h_kv * d if k_stride is None else k_stride, h_kv * d if v_stride is None else v_stride)
+                   k_cache.stride(0), k_cache.stride(1), k_cache.stride(2), row_stride("q", q, q_stride, h_q),
+                   row_stride("k", k, k_stride, h_kv), row_stride("v", v, v_stride, h_kv))
 
 
 class GdnSampleShape(ctypes.Structure):

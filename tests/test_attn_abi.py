@@ -151,3 +151,23 @@ def test_shapes_from_tensors():
     assert (s.n_rows, s.vocab, s.dtype, s.row_stride) == (4, 7, 1, 10)
     with pytest.raises(ValueError):
         gdn.GdnSampleShape.from_logits(x.T)
+
+
+def test_tensors_that_do_not_fit_the_shape_are_refused():
+    import torch
+    table, lens = torch.zeros(3, 5, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    cache = torch.zeros(7, 16, 2, 64)
+    wide = torch.zeros(9, (8 + 2 * 2) * 64 + 16)
+    make = lambda **kw: gdn.GdnAttnShape.from_cache(kw.pop("k_cache", cache), kw.pop("table", table), 8, 9, 4, **kw)
+    s = make(v_cache=cache.clone(), q=wide, k=wide[:, 8 * 64:], v=wide[:, 10 * 64:], seq_lens=lens)
+    assert (s.q_stride, s.k_stride, s.v_stride) == (784, 784, 784)
+    s = make(q=wide[:, :8 * 64].view(9, 8, 64), k=torch.zeros(9, 2, 64), v=wide[:1, 10 * 64:])
+    assert (s.q_stride, s.k_stride, s.v_stride) == (784, 128, 128)
+    assert make(q=wide[:1], q_stride=784).q_stride == 784
+    for wrong in (dict(v_cache=torch.zeros(7, 2, 16, 64).transpose(1, 2)), dict(v_cache=cache.bfloat16()), dict(v_cache=cache[:6]),
+                  dict(table=table.long()), dict(table=torch.zeros(3, 9, dtype=torch.int32)[:, :5]), dict(table=table[0]),
+                  dict(seq_lens=lens.long()), dict(seq_lens=lens[:2]), dict(seq_lens=torch.zeros(6, dtype=torch.int32)[::2]),
+                  dict(q=wide.bfloat16()), dict(q=wide, q_stride=512), dict(q=torch.zeros(9, 8, 128)[..., :64]), dict(q=torch.zeros(9, 4, 64)),
+                  dict(k=wide[:, ::2]), dict(k=wide[:, 11 * 64:11 * 64 + 64]), dict(v=torch.zeros(9, 2, 2, 64))):
+        with pytest.raises(ValueError):
+            make(**wrong)
