@@ -84,6 +84,7 @@ __device__ __noinline__ u64 weigh_any(float x, double m, double per)
 {
     if (!(x > -INFINITY)) return 0;   // (no number, too)
     const double d = (double)x - m;
+    if (d == 0.0) return 1ull << SA_UNIT;   // (a short way for rows of equal logits, whose last bin is bisected)
     return d * per > -SA_DEEP ? units_of_power(d, per) : 0;
 }
 
