@@ -440,6 +440,9 @@ int gdn_attn_decode(const gdn_attn_shape_t *shape, const void *q, const void *k_
  * Attention of the nodes of a draft tree (or of a chunk of a prompt, parent NULL): row i of sequence b sees its seq_lens[b]
  * committed tokens, its ancestors and itself, row j being token seq_lens[b] + j of the cache, where gdn_kv_append put it.
  * Nodes that a row does not see have no influence on it, whatever their values.
+ * (Both calls.)  Scores, maxima, denominators and sums are held in fp32.  bf16 calls with heads of 64 or 128 components round a token's weight
+ * to bf16 before it meets its values (half a step, 2^-8 of it, and up to 1.0e-4 of it more where there are over 64 rows per key/value head);
+ * other calls keep it in fp32.  Outputs are rounded once.
  * (Both calls.)  Among what a row sees, a score that is NaN or +inf makes its output NaN, as inf - inf is none; a score of -inf weighs
  * nothing, and where all of them are -inf the row gets zeros, as one that sees nothing.
  */
@@ -470,7 +473,7 @@ typedef struct gdn_sample_shape {
  *   min_p <= 0 or NaN: off.  A logit of -inf or NaN is never taken; one of +inf is taken before all finite ones.  A row without any logit that
  *   can be taken gives token -1, prob 0.  Weights (exp of the difference to the largest logit / temperature) count in units of
  *   2^-45 of the likeliest one's, each rounded, so that a token of less than half a unit is not taken, and a random number, top_p or
- *   min_p within vocab * 2^-46 of a border may fall on its other side.
+ *   min_p whose border is nearer than vocab * 2^-46 of that weight, or 2e-12 of the sum, may fall on its other side.
  * status_dev is not written by this build.
  */
 int gdn_sample(const gdn_sample_shape_t *shape, const void *logits, const float *temperature, const int32_t *top_k,

@@ -12,8 +12,8 @@
 // Roles: warps 0-3 and 4-7 the rows of the streams, warp 8 the tiles of keys and warp 9 those of values, which warp 11 looks at where
 // not all rows see them, warp 10 the products.  Two or more stages of keys and of values, each with its own barriers.  Pages whose size
 // is a multiple of 8 come by tensor copies, a page or a part of one each, straight into the swizzled layout of the products' operands;
-// others by cp.async, row by row: one warp needs 3300 clocks to issue a tile that way, the products of two streams 2048 (trees of 32
-// sequences: 335 us with pages of 7 tokens, 213 with pages of 16).
+// others by cp.async, row by row, which one warp cannot issue as fast as the products go (trees of 32 sequences: 294 us with pages of 7
+// tokens, 183 with pages of 16).
 // A row's 128 scores stay in its thread's registers (the warps of the rows take over what the others leave).
 // Every wait is bounded; one that expires raises a flag that ends the others.
 #include "gdn_attn.cuh"
@@ -27,9 +27,8 @@ constexpr int AS_M = 256, AS_TN = 128, AS_MOST = 4;
 constexpr float AS_SLACK = 8.f;   // a maximum may rise by this many powers of two before the sums follow
 
 template <int D> __host__ __device__ constexpr int as_tile_bytes() { return AS_TN * D * 2; }
-// Tiles of keys, and of values, on their way or at work: what shared memory holds beside the queries.  (A tile's copy of
-// pages of 24 tokens takes 4000 clocks, the work on a tile 3300: with two tiles of values, and one of them on its way at a time, trees of 32
-// sequences took 250 us, with three 225.)
+// Tiles of keys, and of values, on their way or at work: what shared memory holds beside the queries.  (Trees of 32 sequences: with two tiles
+// of values 187 us on pages of 16 tokens and 196 on pages of 24, with three 183 and 193.)
 template <int D> __host__ __device__ constexpr int as_k_stages() { return D == 128 ? 2 : 4; }
 template <int D> __host__ __device__ constexpr int as_v_stages() { return D == 128 ? 3 : 4; }
 template <int D> __host__ __device__ constexpr size_t as_smem() { return (size_t)as_tile_bytes<D>() * (2 + as_k_stages<D>() + as_v_stages<D>()) + 1024; }

@@ -6,8 +6,9 @@
 // kept weights exceeds u * (their sum).
 //
 // A row belongs to the CTAs of a cluster (one to eight).  They go over it two to four times: from shared memory where a CTA's part is
-// small (few rows: what counts is the time of a pass), else from where the first reading left it, L2 (many rows: what counts is how
-// many CTAs an SM holds; the rows at work at one time are some 100 MB at most).  Nothing is sorted but the
+// small (few rows: what counts is the time of a pass), else from where the first reading left it: L2, while the rows at work at one time
+// fit there (many rows: what counts is how many CTAs an SM holds.  Up to 592 rows are at work at once; 256 of 131071 fp32 logits, 134 MB,
+// take 0.90 us each with top-p, 600 of them 0.84: instructions decide, not where a pass reads from).  Nothing is sorted but the
 // members of one bin: (m - x) / T in units of 1/64 is a bin number that falls as x rises, and one pass counts the tokens of each bin.
 // The first k end in a bin that the counts tell.  Where the p end the counts nearly tell: a count times the weight at the bin's middle
 // is off by a percent at most, so that the next pass, which sums the weights for good, sums them up to that bin, in it and
@@ -35,7 +36,7 @@ constexpr int SA_THREADS = 256, SA_WARPS = SA_THREADS / 32, SA_CTAS = 4;
 constexpr int SA_BINS = 2048, SA_OWN = SA_BINS / SA_THREADS;   // bins, of a thread
 constexpr int SA_HELD = 32 << 10;       // bytes of a row that a CTA holds in shared memory
 constexpr float SA_PER_NAT = 64.f;
-constexpr int SA_SORT = 2048;           // members of a bin that are sorted; more are bisected, which takes some 40 passes: 0.7 ms for 131071 logits
+constexpr int SA_SORT = 2048;           // members of a bin that are sorted; more are bisected, some 40 passes: 131071 equal logits, top-p, take 0.9 ms (256 rows: 6 ms)
 constexpr int SA_UNIT = 45;             // weights in units of 2^-45
 constexpr double SA_DEEP = 60.0;        // logits further below the largest than this many powers of two count as that far: weights of nothing
 typedef unsigned long long u64;
@@ -831,7 +832,8 @@ template <typename T, bool HELD> __global__ void __launch_bounds__(SA_THREADS, H
 
 cudaError_t launch_sample(const SampleParams &p, bool bf16, cudaStream_t stream)
 {
-    // CTAs of a row: as many as are resident at once for all rows together (up to 592), one to eight, none with less than 2048 logits.
+    // CTAs of a row: as many as are resident at once for all rows together (up to 592), one to eight, none with less than about 1024 logits (more
+    // than 2048 are cut into two).
     int ranks = 1;
     while (ranks < 8 && p.vocab > 2048 * ranks && (long long)p.n_rows * ranks * 2 <= SA_CTAS * AT_SMS) ranks *= 2;
     const int chunk = ((p.vocab + ranks - 1) / ranks + 7) / 8 * 8;
